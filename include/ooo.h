@@ -32,6 +32,9 @@
  *   ooo_linear_qk_norm_rope  the q/k/v projection fused with the q/k norms,
  *                      the rotation and the cache writes
  *
+ * ooo_batch.h declares the entry points for a batch of requests over cache
+ * pages, under the same conventions.
+ *
  * Conventions shared by every entry point
  *   - Return value: OOO_OK (0) or a negative ooo_status.  On error nothing has
  *     been enqueued and ooo_last_error() returns a message (thread-local,

@@ -21,7 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libooo.so")
 
-HIP_SOURCES = ["tree_attn.hip", "lmhead.hip", "accept_compact.hip", "layer.hip", "linear.hip"]
+HIP_SOURCES = ["tree_attn.hip", "lmhead.hip", "accept_compact.hip", "layer.hip", "linear.hip", "paged_cache.hip",
+               "paged_attn.hip", "sample.hip"]
 HOST_SOURCES = ["host.cpp"]
 ARCH = "gfx950"
 

@@ -1,4 +1,4 @@
-"""ctypes binding of libooo (C ABI declared in include/ooo.h).
+"""ctypes binding of libooo (C ABI declared in include/ooo.h and ooo_batch.h).
 
 Argument marshalling only: every computation happens in the native library.
 Device arguments are torch tensors on the ROCm device (their ``data_ptr()``
@@ -71,6 +71,30 @@ SIGNATURES = {
 }
 
 
+class PagedBatchStruct(ctypes.Structure):
+    """ooo_paged_batch of include/ooo_batch.h."""
+
+    _fields_ = [("n_seqs", _i32), ("n_rows", _i32), ("row_start", _vp), ("seq_len", _vp), ("page_table", _vp),
+                ("shared_pages", _vp), ("anc_mask", _vp), ("page_stride", _i64), ("table_ld", _i32),
+                ("shared_len", _i32), ("page_rows", _i32), ("n_pages", _i32), ("n_q_heads", _i32),
+                ("n_kv_heads", _i32), ("head_dim", _i32), ("mask_words", _i32), ("dt", ctypes.c_int)]
+
+
+# the same for include/ooo_batch.h (a batch goes in as the struct's address)
+BATCH_SIGNATURES = {
+    "ooo_paged_append": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, ctypes.c_float, _vp, ctypes.c_double, _vp, _vp,
+                                        _vp, _vp]),
+    "ooo_paged_plan_bytes": (_sz, [_vp]),
+    "ooo_paged_plan": (ctypes.c_int, [_vp, _vp, _sz, _vp]),
+    "ooo_paged_attn_workspace": (_sz, [_vp]),
+    "ooo_paged_attn": (ctypes.c_int, [_vp, _vp, _sz, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _sz, _vp]),
+    "ooo_paged_compact": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _vp, _vp, _i32, _vp]),
+    "ooo_sample_workspace": (_sz, [_i32, _i32]),
+    "ooo_sample": (ctypes.c_int, [_vp, _i64, ctypes.c_int, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                  _sz, _vp]),
+}
+
+
 class OooError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"[{status}] {message}")
@@ -86,7 +110,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise OSError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_00814_amd.build`")
         h = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in (*SIGNATURES.items(), *BATCH_SIGNATURES.items()):
             f = getattr(h, name)
             f.restype = res
             f.argtypes = args
@@ -505,3 +529,198 @@ def swiglu(gate_up, out, n_rows: Optional[int] = None, stream=None) -> None:
     _dev(out, "out")
     n = gate_up.shape[0] if n_rows is None else n_rows
     _check(lib().ooo_swiglu(gate_up.data_ptr(), n, out.shape[-1], out.data_ptr(), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------
+# a batch of sequences over cache pages
+
+
+def _on(t, name: str, device, dtype=None, shape=None):
+    """``t`` as a contiguous tensor of ``device`` (the batch's), or a ValueError."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the batch on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {list(shape)}, not {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class PagedBatch:
+    """ooo_paged_batch over torch tensors, which it keeps alive.  Made once
+    for a batch's buffers: the kernels read what the tensors hold when they
+    run, so lengths and page tables may change between calls (the plan is then
+    made anew).
+
+    row_start [n_seqs + 1], seq_len [n_seqs], page_table [n_seqs][table_ld]
+    int32; k_pages [n_pages][Hkv][page_rows][D], one layer's pool (v_pages has
+    its shape and strides; pages may lie apart, as where the pools of several
+    layers are interleaved); n_rows rows of q, qkv and out; shared_pages int32
+    with shared_len tokens, or None; anc_mask [>= n_rows][words] int64, or None."""
+
+    def __init__(self, row_start, seq_len, page_table, k_pages, n_q_heads: int, n_rows: int, shared_pages=None,
+                 shared_len: int = 0, anc_mask=None):
+        import torch
+
+        dev = k_pages.device
+        if dev.type != "cuda":
+            raise ValueError("k_pages must be a device tensor")
+        if k_pages.dim() != 4:
+            raise ValueError("k_pages must be [n_pages][n_kv_heads][page_rows][head_dim]")
+        n_pages, Hkv, rows, D = k_pages.shape
+        n = seq_len.numel()
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [n_seqs][table_ld]")
+        b = PagedBatchStruct()
+        b.row_start = _on(row_start, "row_start", dev, torch.int32, (n + 1,))
+        b.seq_len = _on(seq_len, "seq_len", dev, torch.int32, (n,))
+        b.page_table = _on(page_table, "page_table", dev, torch.int32, (n, page_table.shape[1]))
+        if shared_len > 0 and (shared_pages is None or shared_pages.numel() * rows < shared_len):
+            raise ValueError(f"shared_pages cannot hold {shared_len} tokens")
+        b.shared_pages = None if shared_pages is None else _on(shared_pages, "shared_pages", dev, torch.int32)
+        if anc_mask is not None:
+            if anc_mask.dim() != 2 or anc_mask.shape[0] < n_rows or anc_mask.element_size() != 8:
+                raise ValueError(f"anc_mask must be [>= {n_rows}][words] of 64 bits")
+            b.anc_mask = _on(anc_mask, "anc_mask", dev)
+            b.mask_words = anc_mask.shape[1]
+        b.n_seqs, b.n_rows, b.table_ld, b.shared_len = n, n_rows, page_table.shape[1], shared_len
+        b.page_rows, b.n_pages, b.n_q_heads, b.n_kv_heads, b.head_dim = rows, n_pages, n_q_heads, Hkv, D
+        b.dt = dtype_code(k_pages)
+        self.device, self.dtype, self.pool = dev, k_pages.dtype, tuple(k_pages.shape)
+        self.n_seqs, self.n_rows, self.Hq, self.Hkv, self.D = n, n_rows, n_q_heads, Hkv, D
+        b.page_stride = self.page_stride = self._stride_of(k_pages, "k_pages")
+        self._keep = (row_start, seq_len, page_table, shared_pages, anc_mask)
+        self.struct = b
+        self.address = ctypes.addressof(b)
+
+    def _stride_of(self, t, name: str) -> int:
+        n_pages, Hkv, rows, D = self.pool
+        page = Hkv * rows * D
+        if tuple(t.shape[-4:]) != self.pool or tuple(t.stride()[-3:]) != (rows * D, D, 1):
+            raise ValueError(f"{name} must be [{n_pages}][{Hkv}][{rows}][{D}] with contiguous pages")
+        s = t.stride(-4) if n_pages > 1 else max(t.stride(-4), page)
+        if s < page:
+            raise ValueError(f"{name}: pages overlap")
+        return s
+
+    def pool_ptr(self, t, name: str) -> int:
+        """Address of a pool of this batch, after its checks."""
+        if t.device != self.device or t.dtype != self.dtype:
+            raise ValueError(f"{name} must be {self.dtype} on {self.device}")
+        if self._stride_of(t, name) != self.page_stride:
+            raise ValueError(f"{name}: pages lie {t.stride(-4)} elements apart, the batch's {self.page_stride}")
+        return t.data_ptr()
+
+    def row_ptr(self, t, name: str) -> int:
+        return _on(t, name, self.device, self.dtype, (self.n_rows, self.Hq, self.D))
+
+
+def _stream_on(device, stream) -> Optional[int]:
+    """The stream of a call on ``device``: the given one, or the device's current one."""
+    if stream is not None:
+        return _stream(stream)
+    import torch
+
+    current = torch._C._cuda_getDevice()
+    if device.index != current:
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{current}")
+    return torch._C._cuda_getCurrentRawStream(current)
+
+
+def paged_append(batch: PagedBatch, qkv, q_norm, k_norm, eps: float, rope_theta: float, q_out, k_pages, v_pages,
+                 depth=None, stream=None) -> None:
+    """qkv [n_rows][(Hq + 2 Hkv) D], rows may lie apart; q_norm/k_norm [D] or
+    None; depth [n_rows] int32 or None (chains); q_out [n_rows][Hq][D]; k and v
+    go to the new rows' places in one layer's pools."""
+    import torch
+
+    n, width = batch.n_rows, (batch.Hq + 2 * batch.Hkv) * batch.D
+    if qkv.device != batch.device or qkv.dtype != batch.dtype or tuple(qkv.shape) != (n, width) or qkv.stride(1) != 1:
+        raise ValueError(f"qkv must be [{n}][{width}] {batch.dtype} on {batch.device}")
+    norms = [None if t is None else _on(t, nm, batch.device, batch.dtype, (batch.D,))
+             for t, nm in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
+    dp = None if depth is None else _on(depth, "depth", batch.device, torch.int32, (n,))
+    ld = qkv.stride(0) if n > 1 else max(qkv.stride(0), width)
+    _check(lib().ooo_paged_append(batch.address, qkv.data_ptr(), ld, norms[0], norms[1], eps, dp, rope_theta,
+                                  batch.row_ptr(q_out, "q_out"), batch.pool_ptr(k_pages, "k_pages"),
+                                  batch.pool_ptr(v_pages, "v_pages"), _stream_on(batch.device, stream)))
+
+
+def paged_plan_bytes(batch: PagedBatch) -> int:
+    return int(lib().ooo_paged_plan_bytes(batch.address))
+
+
+def paged_plan(batch: PagedBatch, plan=None, stream=None):
+    """The step's plan in ``plan`` (uint8, paged_plan_bytes), or in a new tensor; returns it."""
+    import torch
+
+    if plan is None:
+        plan = torch.empty(max(paged_plan_bytes(batch), 16), dtype=torch.uint8, device=batch.device)
+    _check(lib().ooo_paged_plan(batch.address, _on(plan, "plan", batch.device, torch.uint8), plan.numel(),
+                                _stream_on(batch.device, stream)))
+    return plan
+
+
+def paged_attn_workspace(batch: PagedBatch) -> int:
+    return int(lib().ooo_paged_attn_workspace(batch.address))
+
+
+def paged_attn(batch: PagedBatch, plan, q, k_pages, v_pages, scale: float, out, workspace, stream=None) -> None:
+    """q, out [n_rows][Hq][D]; one layer's pools; plan of ``paged_plan``;
+    workspace of ``paged_attn_workspace`` bytes."""
+    import torch
+
+    ws = _on(workspace, "workspace", batch.device)
+    _check(lib().ooo_paged_attn(batch.address, _on(plan, "plan", batch.device, torch.uint8), plan.numel(),
+                                batch.row_ptr(q, "q"), batch.pool_ptr(k_pages, "k_pages"),
+                                batch.pool_ptr(v_pages, "v_pages"), scale, batch.row_ptr(out, "out"), ws,
+                                workspace.numel() * workspace.element_size(), _stream_on(batch.device, stream)))
+
+
+def paged_compact(batch: PagedBatch, k_pages, v_pages, path, accept_len, stream=None) -> None:
+    """k_pages/v_pages: the pools of all layers, [L][n_pages][Hkv][page_rows][D]
+    (or one layer's); path [n_seqs][path_cap], accept_len [n_seqs] int32."""
+    import torch
+
+    if k_pages.dim() not in (4, 5) or k_pages.dim() != v_pages.dim() or k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages must be [L][n_pages][n_kv_heads][page_rows][head_dim]")
+    many = k_pages.dim() == 5
+    if many and k_pages.stride(0) != v_pages.stride(0):
+        raise ValueError("k_pages and v_pages must have the same strides")
+    if path.dim() != 2:
+        raise ValueError("path must be [n_seqs][path_cap]")
+    cap = path.shape[1]
+    _check(lib().ooo_paged_compact(batch.address, batch.pool_ptr(k_pages, "k_pages"),
+                                   batch.pool_ptr(v_pages, "v_pages"), k_pages.shape[0] if many else 1,
+                                   k_pages.stride(0) if many else 0,
+                                   _on(path, "path", batch.device, torch.int32, (batch.n_seqs, cap)),
+                                   _on(accept_len, "accept_len", batch.device, torch.int32, (batch.n_seqs,)), cap,
+                                   _stream_on(batch.device, stream)))
+
+
+def sample_workspace(n_rows: int, vocab: int) -> int:
+    return int(lib().ooo_sample_workspace(n_rows, vocab))
+
+
+def sample(logits, u, ids, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, kept=None,
+           stream=None) -> None:
+    """One token per row: logits [rows][V] float32 or bf16 (rows may lie
+    apart); u float32, ids int32 [rows]; the settings [rows] (top_k int32, the
+    others float32) or None; prob float32, kept int32 [rows] or None."""
+    import torch
+
+    dev = logits.device
+    if dev.type != "cuda" or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a device tensor [rows][vocab] with contiguous rows")
+    n, V = logits.shape
+    f, i = torch.float32, torch.int32
+    args = [None if t is None else _on(t, nm, dev, dt, (n,))
+            for t, nm, dt in ((temperature, "temperature", f), (top_k, "top_k", i), (top_p, "top_p", f),
+                              (min_p, "min_p", f), (u, "u", f), (ids, "ids", i), (prob, "prob", f),
+                              (kept, "kept", i))]
+    ld = logits.stride(0) if n > 1 else max(logits.stride(0), V)
+    _check(lib().ooo_sample(logits.data_ptr(), ld, dtype_code(logits), n, V, *args,
+                            _on(workspace, "workspace", dev), workspace.numel() * workspace.element_size(),
+                            _stream_on(dev, stream)))
