@@ -7,14 +7,11 @@
 // outputs O: O = sum_s exp2(m_s - m) O_s / sum_s exp2(m_s - m) l_s.  That is
 // what lets the shared prompt be read once, for the stacked rows of all
 // sequences, and long sequences be split.  Parts and statistics are float32.
-#include <algorithm>
-
-#include "paged_plan.h"
+#include "paged_attn_bf16.h"
 
 namespace ooo {
 namespace {
 
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 constexpr int kPlanThreads = 1024;
 
 // ------------------------------------------------------------------- plan
@@ -212,81 +209,8 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, ui
   reinterpret_cast<RowSlots*>(plan + s.off_rows)[x] = o;
 }
 
-// -------------------------------------------------------------- attention
-struct AttnArgs {
-  Paged p;
-  PlanHead want;        // key to compare with
-  const uint8_t* plan;
-  long long off_items, off_rows;
-  const void* q;
-  const void* k;
-  const void* v;
-  void* out;
-  float* part_o;        // [slot][Hkv] groups in fragment order
-  float* part_ml;       // [slot][Hkv][group] (m, l)
-  long long max_slots;
-  float scale_log2e;
-};
-
-__device__ __forceinline__ bool plan_fits(const PlanHead& h, const PlanHead& want) {
-  bool ok = true;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ok = ok && h.key[i] == want.key[i];
-  return ok;
-}
-
-// Keys lo .. lo + 63 that the row sees, as bits.  len: own committed tokens;
-// i: the row's index in its sequence; row: its global index.
-__device__ __forceinline__ uint64_t below(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
-__device__ __forceinline__ uint64_t seen(const Paged& p, const Item& it, int i, int row, int lo) {
-  if (it.flags & kShared) return below(it.limit - lo);
-  if (!p.W) return below(min(it.limit, it.len + i + 1) - lo);
-  const int off = lo - it.len;  // index among the new rows of key lo
-  uint64_t w = off < 0 ? below(-off) : 0;
-  const uint64_t* m = p.mask + (size_t)row * p.W;
-  if (off > -64) {
-    const int a = off >> 6, sh = off & 63;  // floor division: a may be -1
-    const uint64_t x0 = a >= 0 && a < p.W ? m[a] : 0, x1 = a + 1 < p.W && a + 1 >= 0 ? m[a + 1] : 0;
-    w |= sh ? (x0 >> sh) | (x1 << (64 - sh)) : x0;
-  }
-  return w & below(it.limit - lo);
-}
-// First key that not every row of the block sees.
-__device__ __forceinline__ int all_see(const Paged& p, const Item& it) {
-  if (it.flags & kShared) return it.limit;
-  return p.W ? it.len : min(it.limit, it.len + it.q0 / p.G + 1);
-}
-
-// Pages of one item: page of key t, or -1.
-struct Pages {
-  const int32_t* ids;
-  int shift, n_pages;
-  __device__ __forceinline__ Pages(const Paged& p, const Item& it)
-      : ids(it.flags & kShared ? p.shared_pages : p.table + (size_t)it.seq * p.table_ld),
-        shift(p.page_shift),
-        n_pages(p.n_pages) {}
-  __device__ __forceinline__ int at(int t, bool& bad) const {
-    const int id = ids[t >> shift];
-    const bool ok = id >= 0 && id < n_pages;
-    bad = bad || !ok;
-    return ok ? id : 0;
-  }
-};
-
-template <class T>
-__device__ __forceinline__ f32x4 load4(const T* p);
-template <>
-__device__ __forceinline__ f32x4 load4<float>(const float* p) {
-  return *reinterpret_cast<const f32x4u*>(p);
-}
-template <>
-__device__ __forceinline__ f32x4 load4<uint16_t>(const uint16_t* p) {
-  const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-  return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
-               __uint_as_float(v[1] & 0xFFFF0000u)};
-}
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)(pack_bf16x2(v, 0.f) & 0xFFFFu); }
+// ------------------------------------------------------ attention, float32
+__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
 // One item of up to 16 query rows on the f32 matrix instruction (16x16x4).
 // The keys go in tiles of 16, dealt round-robin to the waves; a wave computes
@@ -296,18 +220,18 @@ __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)(p
 // order (lane (c, q) holds row c's scores of keys 4q .. 4q + 3).  Lane (c, q)
 // of the O^T accumulator dt holds row c, columns 64 (dt / 4) + 16 q + 4 r +
 // dt % 4.
-template <class T, int D>
-__global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
+template <int D>
+__global__ __launch_bounds__(64 * 1024 / D) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int NW = 1024 / D;
   constexpr int KS = D / 16;
   __shared__ f32x4 o_s[NW][KS][64];
   __shared__ f32x2_t ml_s[NW][16];
   __shared__ int odd_s[NW];
   const Paged& p = a.p;
-  const PlanHead* head = reinterpret_cast<const PlanHead*>(a.plan);
   const int g = blockIdx.x % p.Hkv, item = blockIdx.x / p.Hkv;
-  if (!plan_fits(*head, a.want) || item >= head->items) return;
-  const Item it = reinterpret_cast<const Item*>(a.plan + a.off_items)[item];
+  const PlanHead head = load_head(a);
+  const Item it = load_item(a, item);  // within the plan's bound whatever it holds
+  if (!plan_fits(head, a.want) || item >= head.items) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, qd = lane >> 4;
   const bool on = c < it.nq;
@@ -315,24 +239,24 @@ __global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
   const long long row = (long long)it.row0 + i;
   const Pages pages(p, it);
   const int head_off = g << p.page_shift, in_page = (1 << p.page_shift) - 1;
-  const T* const kp = (const T*)a.k;
-  const T* const vp = (const T*)a.v;
+  const float* const kp = (const float*)a.k;
+  const float* const vp = (const float*)a.v;
   const int s0 = 4 * it.t0, s1 = min(4 * it.t1, (it.limit + 15) / 16);
   const int all = all_see(p, it);
   bool bad = false;
 
   f32x4 qv[KS], kv[KS];
-  const T* const qrow = (const T*)a.q + (row * p.Hq + head_q) * D + 4 * qd;
+  const float* const qrow = (const float*)a.q + (row * p.Hq + head_q) * D + 4 * qd;
 #pragma unroll
-  for (int s = 0; s < KS; ++s) qv[s] = load4<T>(qrow + 16 * s) * a.scale_log2e;
+  for (int s = 0; s < KS; ++s) qv[s] = load4(qrow + 16 * s) * a.scale_log2e;
   // rows past the keys re-read the last one (weight zero)
   const auto tile_base = [&](int t) {
     return (long long)pages.at(16 * t, bad) * p.page_stride + ((long long)head_off + ((16 * t) & in_page)) * D;
   };
   const auto load_k = [&](int t) {
-    const T* kr = kp + tile_base(t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
+    const float* kr = kp + tile_base(t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kv[s] = load4<T>(kr + 16 * s);
+    for (int s = 0; s < KS; ++s) kv[s] = load4(kr + 16 * s);
   };
   f32x4 o[KS];
 #pragma unroll
@@ -342,12 +266,12 @@ __global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
   for (int t = s0 + wave; t < s1; t += NW) {
     const int lo = 16 * t;
     f32x4 vv[4][D / 64];
-    const T* const vb = vp + tile_base(t);
+    const float* const vb = vp + tile_base(t);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int h = 0; h < D / 64; ++h)
-        vv[r][h] = load4<T>(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
+        vv[r][h] = load4(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
     f32x4 score = {0.f, 0.f, 0.f, 0.f};
     // chains of eight products added in a tree: few roundings in a row
 #pragma unroll
@@ -428,22 +352,22 @@ __global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
       const uint64_t mw = seen(p, it, i, (int)row, lo);
 #pragma unroll 1
       for (int j = 0; j < 16 && lo + j < it.limit; ++j) {
-        const T* kr = kp + tb + (size_t)j * D + 4 * qd;
+        const float* kr = kp + tb + (size_t)j * D + 4 * qd;
         f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) s4 += load4<T>(kr + 16 * s) * (load4<T>(qrow + 16 * s) * a.scale_log2e);
+        for (int s = 0; s < KS; ++s) s4 += load4(kr + 16 * s) * (load4(qrow + 16 * s) * a.scale_log2e);
         float sc = (s4[0] + s4[1]) + (s4[2] + s4[3]);
         sc += shfl_xor_f(sc, 16);
         sc += shfl_xor_f(sc, 32);
         const float pk = (mw >> j) & 1ull ? exp2f(sc - base) : 0.f;
         if (pk == 0.f) continue;
         l_run += pk;
-        const T* vr = vp + tb + (size_t)j * D + 16 * qd;
+        const float* vr = vp + tb + (size_t)j * D + 16 * qd;
 #pragma unroll
         for (int h = 0; h < D / 64; ++h)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const f32x4 x = load4<T>(vr + 64 * h + 4 * e);
+            const f32x4 x = load4(vr + 64 * h + 4 * e);
 #pragma unroll
             for (int d4 = 0; d4 < 4; ++d4) o[4 * h + d4][e] += pk * x[d4];
           }
@@ -466,9 +390,9 @@ __global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
   if (poison) den = __builtin_nanf("");
   if (it.flags & kDirect) {
     const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees no key is zero
-    T* orow = (T*)a.out + (row * p.Hq + head_q) * D + 64 * (wave >> 2) + 16 * qd + (wave & 3);
+    float* orow = (float*)a.out + (row * p.Hq + head_q) * D + 64 * (wave >> 2) + 16 * qd + (wave & 3);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) store1(orow + 4 * r, acc[r] * inv);
+    for (int r = 0; r < 4; ++r) orow[4 * r] = acc[r] * inv;
   } else if (it.slot < a.max_slots) {
     const size_t sl = (size_t)it.slot * p.Hkv + g;
     reinterpret_cast<f32x4*>(a.part_o)[(sl * KS + wave) * 64 + lane] = acc;
@@ -477,25 +401,36 @@ __global__ __launch_bounds__(64 * 1024 / D) void attn_f32_kernel(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------- join
-// One wave per (16 stacked query rows, KV head, accumulator piece): lane (c,
-// q) joins 4 columns of row c over the row's shared and own slots.
+// One wave per (group of stacked query rows, KV head, accumulator piece): a
+// lane joins 4 columns of one row over the row's shared and own slots.  Lane
+// (c, q) of a piece holds row c and, in float32 (groups of 16), columns 64
+// (piece / 4) + 16 q + 4 e + piece % 4; in bf16 (groups of 32) columns
+// 8 piece + 4 q + e.
 template <class T, int D>
-__global__ __launch_bounds__(64) void join_kernel(AttnArgs a, int pieces) {
-  constexpr int KS = D / 16;
+__global__ __launch_bounds__(64) void join_kernel(PagedAttnArgs a) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int GR = BF ? 32 : 16, NP = D * GR / 256;
   const Paged& p = a.p;
-  const PlanHead* head = reinterpret_cast<const PlanHead*>(a.plan);
-  const int lane = threadIdx.x, c = lane & 15, qd = lane >> 4;
+  const PlanHead head = load_head(a);
+  const int lane = threadIdx.x, c = lane % GR, qd = lane / GR;
   int w = blockIdx.x;
-  const int dt = w % KS;
-  w /= KS;
-  const int g = w % p.Hkv, x = (w / p.Hkv) * 16 + c;
+  const int pc = w % NP;
+  w /= NP;
+  const int g = w % p.Hkv, x = (w / p.Hkv) * GR + c;
   const int i = x / p.G, h = g * p.G + x - i * p.G;
-  const bool fits = plan_fits(*head, a.want);
-  if (i >= (fits ? head->rows : min(p.row_start[p.n_seqs], p.n_rows))) return;
-  T* orow = (T*)a.out + ((size_t)i * p.Hq + h) * D + 64 * (dt >> 2) + 16 * qd + (dt & 3);
-  if (!fits) {
+  const bool fits = plan_fits(head, a.want);
+  if (i >= (fits ? head.rows : min(p.row_start[p.n_seqs], p.n_rows))) return;
+  T* const orow = (T*)a.out + ((size_t)i * p.Hq + h) * D;
+  const auto put = [&](f32x4 o) {
+    if constexpr (BF)
+      *reinterpret_cast<u32x2*>(orow + 8 * pc + 4 * qd) = u32x2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+    else
 #pragma unroll
-    for (int r = 0; r < 4; ++r) store1(orow + 4 * r, __builtin_nanf(""));
+      for (int e = 0; e < 4; ++e) orow[64 * (pc >> 2) + 16 * qd + 4 * e + (pc & 3)] = o[e];
+  };
+  if (!fits) {
+    const float nan = __builtin_nanf("");
+    put(f32x4{nan, nan, nan, nan});
     return;
   }
   const RowSlots rs = reinterpret_cast<const RowSlots*>(a.plan + a.off_rows)[x];
@@ -504,8 +439,8 @@ __global__ __launch_bounds__(64) void join_kernel(AttnArgs a, int pieces) {
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const auto add = [&](long long slot, int rw) {
     const size_t sl = (size_t)min(slot, a.max_slots - 1) * p.Hkv + g;
-    const f32x2_t ml = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * 16 + rw];
-    const f32x4 o = reinterpret_cast<const f32x4*>(a.part_o)[(sl * KS + dt) * 64 + 16 * qd + rw];
+    const f32x2_t ml = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * GR + rw];
+    const f32x4 o = reinterpret_cast<const f32x4*>(a.part_o)[(sl * NP + pc) * 64 + GR * qd + rw];
     const float mn = fmaxf(m, ml[0]), base = mn == -INFINITY ? 0.f : mn;
     const float wa = exp2f(m - base), wb = exp2f(ml[0] - base);
     den = den * wa + ml[1] * wb;
@@ -513,20 +448,20 @@ __global__ __launch_bounds__(64) void join_kernel(AttnArgs a, int pieces) {
     if (wb > 0.f) acc += o * wb;  // zero times an infinite sum is not zero
     m = mn;
   };
-  const int sb = head->shared_block, sg = sb / 16;
-  for (int s = 0; s < head->shared_splits; ++s)
-    add(head->shared_slot0 + ((long long)(x / sb) * head->shared_splits + s) * sg + (x % sb) / 16, c);
+  const int sb = head.shared_block, sg = sb / GR;
+  for (int s = 0; s < head.shared_splits; ++s)
+    add(head.shared_slot0 + ((long long)(x / sb) * head.shared_splits + s) * sg + (x % sb) / GR, c);
   for (int s = 0; s < rs.splits; ++s) add(rs.slot + (long long)s * rs.stride, rs.row);
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) store1(orow + 4 * r, acc[r] * inv);
+  put(acc * (den == 0.f ? 0.f : 1.f / den));
 }
 
 template <class T, int D>
-void launch_attn(const AttnArgs& a, const PlanShape& s, hipStream_t st) {
-  attn_f32_kernel<T, D><<<(unsigned)(s.max_items * a.p.Hkv), 64 * 1024 / D, 0, st>>>(a);
-  const long long groups = ((long long)a.p.n_rows * a.p.G + 15) / 16;
-  join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D / 16)), 64, 0, st>>>(a, D / 16);
+void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
+  const unsigned items = (unsigned)(s.max_items * a.p.Hkv);
+  if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
+  else paged_attn_f32_kernel<D><<<items, 64 * 1024 / D, 0, st>>>(a);
+  const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
+  join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D * s.group / 256)), 64, 0, st>>>(a);
 }
 
 size_t workspace_bytes(const ooo_paged_batch& b, const PlanShape& s) {
@@ -574,7 +509,7 @@ extern "C" size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch) {
 extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_bytes, const void* q,
                               const void* k_pages, const void* v_pages, float scale, void* out, void* workspace,
                               size_t ws_bytes, void* stream) {
-  AttnArgs a{};
+  PagedAttnArgs a{};
   const int rc = check_paged("ooo_paged_attn", batch, a.p);
   if (rc != OOO_OK) return rc;
   OOO_REQUIRE(plan && q && k_pages && v_pages && out && workspace, OOO_ERR_INVALID, "ooo_paged_attn: null pointer");

@@ -66,11 +66,11 @@ struct RowSlots {
 inline PlanShape plan_shape(const ooo_paged_batch& b) {
   PlanShape s{};
   const bool bf = b.dt == OOO_BF16;
-  s.group = 16;
-  s.narrow = s.wide = 16;
+  s.group = bf ? 32 : 16;
+  s.narrow = s.group;
+  s.wide = bf ? 128 : 16;
   s.cost_narrow = s.cost_wide = 1;
-  s.target = 2 * device_cus() / b.n_kv_heads;
-  (void)bf;
+  s.target = (bf ? 1 : 2) * device_cus() / b.n_kv_heads;
   if (s.target < 1) s.target = 1;
   const long long G = b.n_q_heads / b.n_kv_heads, q = b.n_rows * G;
   const long long stack = b.shared_len > 0 ? (q + s.group - 1) / s.group : 0;
