@@ -206,7 +206,8 @@ int ooo_paged_compact(const ooo_paged_batch* batch, void* k_pages, void* v_pages
  * the largest or finer), so results do not depend on any order of addition.
  *   workspace, ws_bytes   ooo_sample_workspace(n_rows, vocab) bytes (16-byte aligned)
  * Errors: OOO_ERR_INVALID (null pointers, sizes < 1, ld < vocab, unknown
- * dtype), OOO_ERR_UNSUPPORTED (vocab above 2^20), OOO_ERR_CAPACITY, OOO_ERR_HIP.
+ * dtype), OOO_ERR_UNSUPPORTED (vocab above 2^20, n_rows above 65535, workspace
+ * not aligned), OOO_ERR_CAPACITY, OOO_ERR_HIP.
  */
 size_t ooo_sample_workspace(int32_t n_rows, int32_t vocab);
 int ooo_sample(const void* logits, int64_t ld, ooo_dtype dt, int32_t n_rows, int32_t vocab,
