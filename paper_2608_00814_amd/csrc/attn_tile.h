@@ -38,6 +38,14 @@ __device__ __forceinline__ void dma16_nt(const void* base, uint32_t voff, uint32
                : "memory", "m0");
 }
 
+// The same at OFF bytes behind both the source and the LDS address.
+template <int OFF>
+__device__ __forceinline__ void dma16_nt_at(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3 nt" ::"s"(lds), "v"(voff),
+               "s"(base), "n"(OFF)
+               : "memory", "m0");
+}
+
 // Same for 4 bytes per lane (lane l's dword lands at lds + 4*l).
 __device__ __forceinline__ void dma4(const void* base, uint32_t voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(base)
@@ -54,6 +62,15 @@ __device__ __forceinline__ float max3f(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+
+// The end of the wait for a matrix product's result: the compiler knows how
+// long a vector instruction of its own has to stay behind the product that it
+// reads, but not one in inline asm (max3f), which would read what was there
+// before.
+__device__ __forceinline__ void settle(f32x16& s) {
+  const int t = __builtin_amdgcn_readfirstlane(__float_as_int(s[15]));
+  asm volatile("" : "+v"(s) : "s"(t));
 }
 
 // LDS ring geometry for one head_dim.  A tile is 64 rows of K and 64 rows of

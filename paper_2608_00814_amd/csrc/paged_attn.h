@@ -10,7 +10,8 @@ struct PagedAttnArgs {
   Paged p;
   PlanHead want;        // key to compare with
   const uint8_t* plan;
-  long long off_items, off_rows;
+  long long off_blocks, off_first_w, off_first_n, off_items_w, off_items_n, off_rows;
+  int max_items_w, max_items_n, workers;
   const void* q;
   const void* k;
   const void* v;
@@ -27,10 +28,9 @@ struct PagedAttnArgs {
 typedef const __attribute__((address_space(4))) int32_t* ScalarPtr;
 __device__ __forceinline__ ScalarPtr scalar_ptr(const void* p) { return (ScalarPtr)(uintptr_t)p; }
 
-// The workgroup's item, in scalar registers (addresses of the LDS DMA follow
-// from it).
-__device__ __forceinline__ Item load_item(const PagedAttnArgs& a, int item) {
-  const ScalarPtr src = scalar_ptr(a.plan + a.off_items) + (size_t)item * (sizeof(Item) / 4);
+// An item, in scalar registers (addresses of the LDS DMA follow from it).
+__device__ __forceinline__ Item load_item(const uint8_t* items, int item) {
+  const ScalarPtr src = scalar_ptr(items) + (size_t)item * (sizeof(Item) / 4);
   Item it{};
   int* dst = &it.flags;
 #pragma unroll
@@ -46,8 +46,32 @@ __device__ __forceinline__ PlanHead load_head(const PagedAttnArgs& a) {
   PlanHead h{};
   int* dst = h.key;
 #pragma unroll
-  for (int k = 0; k < 13; ++k) dst[k] = src[k];
+  for (int k = 0; k < 16; ++k) dst[k] = src[k];
   return h;
+}
+// The wide items of one worker, in turn: f(item).
+template <class F>
+__device__ __forceinline__ void each_wide(const PagedAttnArgs& a, const PlanHead& h, int worker, F f) {
+  bool first = true;
+  const auto go = [&](int item) __attribute__((always_inline)) {
+    if (!first) __syncthreads();  // the item before is joined
+    first = false;
+    f(item);
+  };
+  int item = worker < h.shared_workers ? worker : h.shared_items, step = h.shared_workers, end = h.shared_items;
+  const int own = worker - h.own_first;
+  bool more = own >= 0 && own < h.own_workers;
+  while (true) {
+    if (item >= end) {
+      if (!more) break;
+      const ScalarPtr fw = scalar_ptr(a.plan + a.off_first_w) + own;
+      item = fw[0], end = min(fw[1], a.max_items_w), step = 1;
+      more = false;
+      continue;
+    }
+    go(item);
+    item += step;
+  }
 }
 __device__ __forceinline__ bool plan_fits(const PlanHead& h, const PlanHead& want) {
   int diff = 0;

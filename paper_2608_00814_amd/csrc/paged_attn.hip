@@ -12,7 +12,8 @@
 namespace ooo {
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 512;
+
 
 // ------------------------------------------------------------------- plan
 // A sequence's rows and own tokens, bounded to what buffers and tables hold.
@@ -26,158 +27,277 @@ __device__ __forceinline__ Seq seq_of(const Paged& p, int b, int R) {
   s.len = min(max(p.seq_len[b], 0), p.own_cap);
   return s;
 }
-__device__ __forceinline__ int blocks_of(const PlanShape& s, int q) {
-  return q <= s.narrow ? (q > 0) : (q + s.wide - 1) / s.wide;
-}
-// keys that query rows up to `last` (of the sequence) can see
-__device__ __forceinline__ int keys_of(const Paged& p, const Seq& s, int last) {
-  const int n = p.W ? min(s.rows, 64 * p.W) : last / p.G + 1;
-  return min(s.len + n, p.own_cap);
-}
-struct Split {
-  int tiles, per, n;
+
+// What a thread of the plan looks at: one shared block, or one sequence.
+struct Entry {
+  Seq q;
+  int rows;     // query rows of all its blocks
+  int block;    // query rows of a block
+  int n;        // blocks
+  bool shared, wide;
+  // block j: its query rows, the keys they can see and its length, in tiles
+  // (wide) or half-tiles
+  __device__ __forceinline__ void at(const Paged& p, int j, int& nq, int& limit, int& len) const {
+    nq = min(block, rows - j * block);
+    if (shared) {
+      limit = p.shared_len;
+    } else {
+      const int last = (j * block + nq - 1) / p.G;
+      limit = min(q.len + (p.W ? min(q.rows, 64 * p.W) : last + 1), p.own_cap);
+    }
+    len = wide ? (limit + kTileKeys - 1) / kTileKeys : (limit + kTileKeys / 2 - 1) / (kTileKeys / 2);
+  }
 };
-__device__ __forceinline__ Split split_of(long long tiles, int cost, long long budget) {
-  const long long n = min(tiles, (tiles * cost + budget - 1) / budget);
-  const long long per = n > 0 ? (tiles + n - 1) / n : 1;
-  return Split{(int)tiles, (int)per, (int)((tiles + per - 1) / per)};
+__device__ __forceinline__ Entry entry_of(const Paged& p, const PlanShape& s, int e, int shared, int sblock, int R) {
+  Entry x;
+  const int stack = R * p.G;
+  x.shared = e < shared;
+  x.q = x.shared ? Seq{0, 0, 0} : seq_of(p, e - shared, R);
+  x.rows = x.shared ? min(sblock, stack - e * sblock) : x.q.rows * p.G;
+  x.wide = x.shared ? sblock > s.narrow : x.rows > s.narrow;
+  x.block = x.wide ? s.wide : s.narrow;
+  x.n = x.rows > 0 ? (x.rows + x.block - 1) / x.block : 0;
+  return x;
 }
 
-// Exclusive scan of two counts over the workgroup; the totals go to every thread.
-__device__ __forceinline__ void scan2(long long& a, long long& b, long long& ta, long long& tb, long long (*sh)[2]) {
+// Exclusive scan of N counts over the workgroup; the totals go to every thread.
+template <int N>
+__device__ __forceinline__ void scan(long long (&v)[N], long long (&total)[N]) {
+  __shared__ long long sh[N][kPlanThreads / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long a0 = a, b0 = b;
-  for (int off = 1; off < 64; off <<= 1) {
-    const long long x = __shfl_up(a, off, 64), y = __shfl_up(b, off, 64);
-    if (lane >= off) a += x, b += y;
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const long long own = v[n];
+    for (int off = 1; off < 64; off <<= 1) {
+      const long long x = __shfl_up(v[n], off, 64);
+      if (lane >= off) v[n] += x;
+    }
+    if (lane == 63) sh[n][wave] = v[n];
+    v[n] -= own;
   }
   __syncthreads();
-  if (lane == 63) sh[wave][0] = a, sh[wave][1] = b;
-  __syncthreads();
-  long long pa = 0, pb = 0;
-  ta = tb = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w == wave) pa = ta, pb = tb;
-    ta += sh[w][0];
-    tb += sh[w][1];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    total[n] = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      if (w < wave) v[n] += sh[n][w];
+      total[n] += sh[n][w];
+    }
   }
-  a += pa - a0;
-  b += pb - b0;
 }
 
-// One workgroup.  First the total cost and the blocks' numbers, then the
-// items and slots of every sequence behind those of the sequences before it.
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, uint8_t* plan) {
-  __shared__ long long sh[kPlanThreads / 64][2];
-  int4* const blocks = reinterpret_cast<int4*>(plan + s.off_blocks);
+// How the workers of a KV head are shared out.
+struct Deal {
+  int splits, shared_workers, own_workers, narrow_workers;
+};
+// Costs in 100 cycles at head_dim 128 (half of them at 64), as measured: a wide
+// tile of a worker; an item's start (its record, pages, queries and first
+// tiles, one behind the other) and end; a half-tile of a narrow worker, whose
+// eight waves have 128 KiB on their way; and a half-tile at the chip's share of
+// the HBM rate.
+constexpr float kCostTile = 21.f, kCostItem = 160.f, kCostHalf = 5.f, kCostHalfHbm = 0.05f;
+
+// Thread 0: the deal that finishes first.  blocks, tiles: of the wide shared
+// part; own: tiles of the sequences' wide blocks; halves: of the narrow blocks.
+__device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int tiles, long long own,
+                             long long halves, bool half_dim) {
+  const int W = s.workers;
+  const float tile = half_dim ? 0.5f * kCostTile : kCostTile, half = half_dim ? 0.5f * kCostHalf : kCostHalf;
+  const float hbm = (half_dim ? 0.5f : 1.f) * kCostHalfHbm * p.Hkv * (float)halves;
+  Deal best{1, 0, 0, 0};
+  float least = INFINITY;
+  const int kinds = (blocks > 0) + (own > 0) + (halves > 0);
+  const float co = (float)own * tile, cn = (float)halves * half;
+  if (W <= kinds) {  // every worker takes a share of everything
+    int n = blocks > 0 ? (W + blocks - 1) / blocks : 1;
+    return Deal{max(min(n, tiles), 1), W, W, W};
+  }
+  for (int n = 1; n <= max(tiles, 1) && (n == 1 || (long long)blocks * (n - 1) <= (long long)kSplitMost * W); ++n) {
+    const int items = blocks * n, room = W - (own > 0) - (halves > 0);
+    const int k0 = (items + room - 1) / room;
+    for (int k = max(k0, 1); k <= k0 + 2; ++k) {
+      const int ws = (items + k - 1) / k, rest = W - ws;
+      int wo = own > 0 ? rest : 0, wn = halves > 0 ? rest : 0;
+      if (own > 0 && halves > 0) {
+        wo = (int)(rest * (co / (co + cn)) + 0.5f);
+        wo = min(max(wo, 1), rest - 1);
+        wn = rest - wo;
+      }
+      float t = blocks > 0 ? k * ((float)((tiles + n - 1) / n) * tile + kCostItem) : 0.f;
+      if (wo > 0) t = fmaxf(t, co / wo + kCostItem);
+      if (wn > 0) t = fmaxf(t, fmaxf(cn / wn, hbm));
+      if (t < least) least = t, best = Deal{n, ws, wo, wn};
+      if (blocks == 0) return best;
+    }
+  }
+  return best;
+}
+
+// One workgroup.  First the lengths, from them the deal, then the items and
+// slots of every entry behind those of the entries before it.
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, int half_dim,
+                                                            uint8_t* plan) {
+  BlockSlots* const blocks = reinterpret_cast<BlockSlots*>(plan + s.off_blocks);
   int* const seq_block = reinterpret_cast<int*>(plan + s.off_seqs);
-  Item* const items = reinterpret_cast<Item*>(plan + s.off_items);
+  int* const first_w = reinterpret_cast<int*>(plan + s.off_first_w);
+  int* const first_n = reinterpret_cast<int*>(plan + s.off_first_n);
+  Item* const items_w = reinterpret_cast<Item*>(plan + s.off_items_w);
+  Item* const items_n = reinterpret_cast<Item*>(plan + s.off_items_n);
+  const int tid = threadIdx.x;
   const int R = min(max(p.row_start[p.n_seqs], 0), p.n_rows);
   const int stack = R * p.G;  // query rows of a KV head
-
-  long long cost = 0, nblk = 0;
-  for (int b0 = 0; b0 < p.n_seqs; b0 += kPlanThreads) {
-    const int b = b0 + threadIdx.x;
-    long long c = 0, n = 0;
-    if (b < p.n_seqs) {
-      const Seq q = seq_of(p, b, R);
-      const int rows = q.rows * p.G;
-      n = blocks_of(s, rows);
-      const bool wide = rows > s.narrow;
-      for (int j = 0; j < n; ++j) {
-        const int last = wide ? min((j + 1) * s.wide, rows) - 1 : rows - 1;
-        c += (long long)((keys_of(p, q, last) + kTileKeys - 1) / kTileKeys) * (wide ? s.cost_wide : s.cost_narrow);
-      }
-    }
-    long long at = n, tc, tn;
-    scan2(at, c, tn, tc, sh);
-    if (b < p.n_seqs) seq_block[b] = (int)(nblk + at);
-    cost += tc;
-    nblk += tn;
-  }
   const bool swide = stack > s.narrow;
-  const int sblock = swide ? s.wide : s.narrow, scost = swide ? s.cost_wide : s.cost_narrow;
-  const int sblocks = p.shared_len > 0 ? (stack + sblock - 1) / sblock : 0;
-  const long long stiles = (p.shared_len + kTileKeys - 1) / kTileKeys;
-  cost += sblocks * stiles * scost;
-  const long long budget = max((cost + s.target - 1) / s.target, 1ll);
-  const Split ss = split_of(sblocks ? stiles : 0, scost, budget);
-  const int sgroups = sblock / s.group;
-  if (threadIdx.x == 0) seq_block[p.n_seqs] = (int)nblk;
+  const int sblock = swide ? s.wide : s.narrow;
+  const int sblocks = p.shared_len > 0 && stack > 0 ? (stack + sblock - 1) / sblock : 0;
+  // entries: a narrow shared block, then the sequences
+  const int lead = swide ? 0 : sblocks, entries = lead + p.n_seqs;
+  const int tiles = (p.shared_len + kTileKeys - 1) / kTileKeys, per_wide = s.wide / s.group;
+  // what an item's start and end cost, in wide tiles and in half-tiles of a wave
+  const int lead_w = half_dim ? 16 : 8, lead_n = half_dim ? 6 : 3;
+  __shared__ Deal deal_s;
 
-  // shared items: all row blocks of a run of tiles next to each other
-  long long item0 = (long long)sblocks * ss.n, slot0 = item0 * sgroups;
-  for (int k = threadIdx.x; k < item0; k += kPlanThreads) {
-    const int sp = k / sblocks, blk = k - sp * sblocks;
-    Item it{};
-    it.flags = kShared | (swide ? kWide : 0);
-    it.q0 = blk * sblock;
-    it.nq = min(sblock, stack - it.q0);
-    it.t0 = sp * ss.per;
-    it.t1 = min(it.t0 + ss.per, ss.tiles);
-    it.limit = it.len = p.shared_len;
-    it.slot = (blk * ss.n + sp) * sgroups;
-    if (k < s.max_items) items[k] = it;
-  }
-  for (int b0 = 0; b0 < p.n_seqs; b0 += kPlanThreads) {
-    const int b = b0 + threadIdx.x;
-    long long ni = 0, ns = 0;
-    Seq q{};
-    int n = 0, rows = 0;
-    if (b < p.n_seqs) {
-      q = seq_of(p, b, R);
-      rows = q.rows * p.G;
-      n = blocks_of(s, rows);
-    }
-    const bool wide = rows > s.narrow;
-    const int block = wide ? s.wide : s.narrow;
-    const auto split = [&](int j, int& nq, int& limit) {
-      nq = min(block, rows - j * block);
-      limit = keys_of(p, q, j * block + nq - 1);
-      return split_of((limit + kTileKeys - 1) / kTileKeys, wide ? s.cost_wide : s.cost_narrow, budget);
-    };
-    for (int j = 0; j < n; ++j) {
-      int nq, limit;
-      const Split sp = split(j, nq, limit);
-      ni += sp.n;
-      if (sblocks || sp.n > 1) ns += (long long)sp.n * ((nq + s.group - 1) / s.group);
-    }
-    long long ti, ts;
-    scan2(ni, ns, ti, ts, sh);
-    long long item = item0 + ni, slot = slot0 + ns;
-    for (int j = 0; j < n; ++j) {
-      int nq, limit;
-      const Split sp = split(j, nq, limit);
-      const bool direct = !sblocks && sp.n == 1;
-      const int groups = (nq + s.group - 1) / s.group;
-      const long long blk = seq_block[b] + j;
-      if (blk < s.max_blocks) blocks[blk] = make_int4((int)slot, direct ? 0 : sp.n, groups, 0);
-      for (int k = 0; k < sp.n; ++k, ++item) {
-        Item it{};
-        it.flags = (wide ? kWide : 0) | (direct ? kDirect : 0);
-        it.seq = b;
-        it.row0 = q.row0;
-        it.q0 = j * block;
-        it.nq = nq;
-        it.t0 = k * sp.per;
-        it.t1 = min(it.t0 + sp.per, sp.tiles);
-        it.limit = limit;
-        it.len = q.len;
-        it.rows = q.rows;
-        it.slot = (int)slot;
-        if (!direct) slot += groups;
-        if (item < s.max_items) items[item] = it;
+  long long all[3] = {0, 0, swide ? sblocks : 0};  // own wide tiles, narrow half-tiles, blocks
+  for (int e0 = 0; e0 < entries; e0 += kPlanThreads) {
+    long long v[3] = {0, 0, 0}, t[3];
+    const int e = e0 + tid;
+    if (e < entries) {
+      const Entry x = entry_of(p, s, e, lead, sblock, R);
+      v[2] = x.n;
+      for (int j = 0; j < x.n; ++j) {
+        int nq, limit, len;
+        x.at(p, j, nq, limit, len);
+        v[x.wide ? 0 : 1] += len + (x.wide ? lead_w : lead_n);
       }
     }
-    item0 += ti;
-    slot0 += ts;
+    scan<3>(v, t);
+    if (e >= lead && e < entries) seq_block[e - lead] = (int)(all[2] + v[2]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) all[k] += t[k];
   }
-  if (threadIdx.x == 0) {
-    head.items = (int)min(item0, s.max_items);
+  const int wblocks = swide ? sblocks : 0;
+  if (tid == 0) deal_s = deal_workers(p, s, wblocks, tiles, all[0], all[1], half_dim != 0);
+  __syncthreads();
+  const Deal d = deal_s;
+  const int runs_w = max(d.own_workers, 1), runs_n = max(d.narrow_workers, 1) * max(s.waves, 1);
+  const long long len_w = max((all[0] + runs_w - 1) / runs_w, 1ll), len_n = max((all[1] + runs_n - 1) / runs_n, 1ll);
+
+  // the wide shared blocks' items, and their slots block by block
+  const int per = (tiles + d.splits - 1) / d.splits, splits = wblocks ? (tiles + per - 1) / per : 0;
+  const int shared_items = wblocks * splits;
+  for (int k = tid; k < shared_items; k += kPlanThreads) {
+    const int sp = k / wblocks, b = k - sp * wblocks;
+    Item it{};
+    it.flags = kShared;
+    it.q0 = b * sblock;
+    it.nq = min(sblock, stack - it.q0);
+    it.t0 = sp * per;
+    it.t1 = min(it.t0 + per, tiles);
+    it.limit = it.len = p.shared_len;
+    it.slot = (b * splits + sp) * per_wide;
+    if (k < s.max_items_w) items_w[k] = it;
+    if (sp == 0 && b < s.max_blocks) blocks[b] = BlockSlots{it.slot, splits, per_wide, 0};
+  }
+
+  // wide and narrow position, wide and narrow items, slots
+  long long at[5] = {0, 0, shared_items, 0, (long long)shared_items * per_wide};
+  long long blk = wblocks;
+  for (int e0 = 0; e0 < entries; e0 += kPlanThreads) {
+    const int e = e0 + tid;
+    Entry x{};
+    long long pos[3] = {0, 0, 0}, tp[3];
+    if (e < entries) {
+      x = entry_of(p, s, e, lead, sblock, R);
+      pos[2] = x.n;
+      for (int j = 0; j < x.n; ++j) {
+        int nq, limit, len;
+        x.at(p, j, nq, limit, len);
+        pos[x.wide ? 0 : 1] += len + (x.wide ? lead_w : lead_n);
+      }
+    }
+    scan<3>(pos, tp);
+    const long long run = x.wide ? len_w : len_n;
+    const int ahead = x.wide ? lead_w : lead_n;
+    // items of a block from position q on: one for each run that it has a part
+    // in, but none for a run that ends in its first `ahead` positions
+    const auto pieces = [&](long long q, int len) {
+      const int k = (int)((q + ahead + len - 1) / run - q / run) + 1;
+      const long long in_lead = (q + ahead) / run - q / run;  // runs that end there
+      return k - (int)in_lead;
+    };
+    long long p0 = x.wide ? at[0] + pos[0] : at[1] + pos[1];
+    long long n[3] = {0, 0, 0}, tn[3];  // wide items, narrow items, slots
+    {
+      long long q = p0;
+      for (int j = 0; j < x.n; ++j) {
+        int nq, limit, len;
+        x.at(p, j, nq, limit, len);
+        const int k = pieces(q, len);
+        n[x.wide ? 0 : 1] += k;
+        if (sblocks || k > 1) n[2] += (long long)k * ((nq + s.group - 1) / s.group);
+        q += ahead + len;
+      }
+    }
+    scan<3>(n, tn);
+    long long item = x.wide ? at[2] + n[0] : at[3] + n[1], slot = at[4] + n[2];
+    Item* const items = x.wide ? items_w : items_n;
+    int* const first = x.wide ? first_w : first_n;
+    const long long most = x.wide ? s.max_items_w : s.max_items_n;
+    for (int j = 0; j < x.n; ++j) {
+      int nq, limit, len;
+      x.at(p, j, nq, limit, len);
+      const int k = pieces(p0, len);
+      const bool direct = !sblocks && k == 1;
+      const int groups = (nq + s.group - 1) / s.group;
+      const long long b = blk + pos[2] + j;
+      if (b < s.max_blocks) blocks[b] = BlockSlots{(int)slot, direct ? 0 : k, groups, 0};
+      Item it{};
+      it.flags = (x.shared ? kShared : 0) | (direct ? kDirect : 0);
+      it.seq = x.shared ? 0 : e - lead;
+      it.row0 = x.q.row0;
+      it.q0 = j * x.block;
+      it.nq = nq;
+      it.limit = limit;
+      it.len = x.shared ? limit : x.q.len;
+      it.rows = x.q.rows;
+      const long long t0 = p0 + ahead, p1 = t0 + len;  // position of the first tile, of the end
+      for (long long q = p0; q < p1;) {
+        const long long r = q / run, end = min((r + 1) * run, p1);
+        if (q == r * run) first[r] = (int)item;  // r < the runs there are
+        if (end > t0) {
+          it.t0 = (int)max(q - t0, 0ll);
+          it.t1 = (int)(end - t0);
+          it.slot = (int)slot;
+          if (!direct) slot += groups;
+          if (item < most) items[item] = it;
+          ++item;
+        }
+        q = end;
+      }
+      p0 = p1;
+    }
+    at[0] += tp[0];
+    at[1] += tp[1];
+    blk += tp[2];
+    at[2] += tn[0];
+    at[3] += tn[1];
+    at[4] += tn[2];
+  }
+  __syncthreads();
+  // runs behind the last item are empty
+  for (int r = (int)((all[0] + len_w - 1) / len_w) + tid; r <= s.workers; r += kPlanThreads) first_w[r] = (int)at[2];
+  for (int r = (int)((all[1] + len_n - 1) / len_n) + tid; r <= s.waves * s.workers; r += kPlanThreads)
+    first_n[r] = (int)at[3];
+  if (tid == 0) {
+    const bool together = d.shared_workers + d.own_workers + d.narrow_workers > s.workers;
     head.rows = R;
-    head.shared_splits = sblocks ? ss.n : 0;
-    head.shared_block = sblock;
-    head.shared_slot0 = 0;
+    head.shared_block = sblocks ? sblock : 0;
+    head.shared_items = (int)min((long long)shared_items, s.max_items_w);
+    head.shared_workers = wblocks ? d.shared_workers : 0;
+    head.own_first = together ? 0 : d.shared_workers;
+    head.own_workers = d.own_workers;
+    head.narrow_first = together ? 0 : d.shared_workers + d.own_workers;
+    head.narrow_workers = s.waves ? d.narrow_workers : 0;
     *reinterpret_cast<PlanHead*>(plan) = head;
   }
 }
@@ -201,9 +321,9 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, ui
     const int block = rows > s.narrow ? s.wide : s.narrow;
     const long long blk = reinterpret_cast<const int*>(plan + s.off_seqs)[lo] + at / block;
     if (blk < s.max_blocks) {
-      const int4 d = reinterpret_cast<const int4*>(plan + s.off_blocks)[blk];
+      const BlockSlots d = reinterpret_cast<const BlockSlots*>(plan + s.off_blocks)[blk];
       const int in = at % block;
-      o = RowSlots{d.x + in / s.group, d.y, d.z, in % s.group};
+      o = RowSlots{d.slot + in / s.group, d.splits, d.groups, in % s.group};
     }
   }
   reinterpret_cast<RowSlots*>(plan + s.off_rows)[x] = o;
@@ -221,183 +341,185 @@ __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cas
 // of the O^T accumulator dt holds row c, columns 64 (dt / 4) + 16 q + 4 r +
 // dt % 4.
 template <int D>
-__global__ __launch_bounds__(64 * 1024 / D) void paged_attn_f32_kernel(PagedAttnArgs a) {
-  constexpr int NW = 1024 / D;
+__global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
+  constexpr int NW = 8;
   constexpr int KS = D / 16;
   __shared__ f32x4 o_s[NW][KS][64];
   __shared__ f32x2_t ml_s[NW][16];
   __shared__ int odd_s[NW];
   const Paged& p = a.p;
-  const int g = blockIdx.x % p.Hkv, item = blockIdx.x / p.Hkv;
+  const int g = blockIdx.x % p.Hkv, worker = blockIdx.x / p.Hkv;
   const PlanHead head = load_head(a);
-  const Item it = load_item(a, item);  // within the plan's bound whatever it holds
-  if (!plan_fits(head, a.want) || item >= head.items) return;
+  if (!plan_fits(head, a.want)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, qd = lane >> 4;
-  const bool on = c < it.nq;
-  const int qi = it.q0 + min(c, it.nq - 1), i = qi / p.G, head_q = g * p.G + qi - i * p.G;
-  const long long row = (long long)it.row0 + i;
-  const Pages pages(p, it);
-  const int head_off = g << p.page_shift, in_page = (1 << p.page_shift) - 1;
-  const float* const kp = (const float*)a.k;
-  const float* const vp = (const float*)a.v;
-  const int s0 = 4 * it.t0, s1 = min(4 * it.t1, (it.limit + 15) / 16);
-  const int all = all_see(p, it);
-  bool bad = false;
+  each_wide(a, head, worker, [&](int item) {
+    const Item it = load_item(a.plan + a.off_items_w, item);
+    const bool on = c < it.nq;
+    const int qi = it.q0 + min(c, it.nq - 1), i = qi / p.G, head_q = g * p.G + qi - i * p.G;
+    const long long row = (long long)it.row0 + i;
+    const Pages pages(p, it);
+    const int head_off = g << p.page_shift, in_page = (1 << p.page_shift) - 1;
+    const float* const kp = (const float*)a.k;
+    const float* const vp = (const float*)a.v;
+    const int s0 = 4 * it.t0, s1 = min(4 * it.t1, (it.limit + 15) / 16);
+    const int all = all_see(p, it);
+    bool bad = false;
 
-  f32x4 qv[KS], kv[KS];
-  const float* const qrow = (const float*)a.q + (row * p.Hq + head_q) * D + 4 * qd;
+    f32x4 qv[KS], kv[KS];
+    const float* const qrow = (const float*)a.q + (row * p.Hq + head_q) * D + 4 * qd;
 #pragma unroll
-  for (int s = 0; s < KS; ++s) qv[s] = load4(qrow + 16 * s) * a.scale_log2e;
-  // rows past the keys re-read the last one (weight zero)
-  const auto tile_base = [&](int t) {
-    return (long long)pages.at(16 * t, bad) * p.page_stride + ((long long)head_off + ((16 * t) & in_page)) * D;
-  };
-  const auto load_k = [&](int t) {
-    const float* kr = kp + tile_base(t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
+    for (int s = 0; s < KS; ++s) qv[s] = load4(qrow + 16 * s) * a.scale_log2e;
+    // rows past the keys re-read the last one (weight zero)
+    const auto tile_base = [&](int t) {
+      return (long long)pages.at(16 * t, bad) * p.page_stride + ((long long)head_off + ((16 * t) & in_page)) * D;
+    };
+    const auto load_k = [&](int t) {
+      const float* kr = kp + tile_base(t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kv[s] = load4(kr + 16 * s);
-  };
-  f32x4 o[KS];
-#pragma unroll
-  for (int dt = 0; dt < KS; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY, l_run = 0.f;
-  if (s0 + wave < s1) load_k(s0 + wave);
-  for (int t = s0 + wave; t < s1; t += NW) {
-    const int lo = 16 * t;
-    f32x4 vv[4][D / 64];
-    const float* const vb = vp + tile_base(t);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int h = 0; h < D / 64; ++h)
-        vv[r][h] = load4(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
-    f32x4 score = {0.f, 0.f, 0.f, 0.f};
-    // chains of eight products added in a tree: few roundings in a row
-#pragma unroll
-    for (int s = 0; s < KS; s += 4) {
-      f32x4 sc[8];
-#pragma unroll
-      for (int ch = 0; ch < 8; ++ch) sc[ch] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int ch = 0; ch < 8; ++ch) {
-          const int x = s + ch / 2, e = 2 * (ch & 1) + j;
-          sc[ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[x][e], qv[x][e], sc[ch], 0, 0, 0);
-        }
-      score += ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
-    }
-    if (t + NW < s1) load_k(t + NW);
-    uint64_t mw = ~0ull;
-    if (lo + 16 > all) mw = seen(p, it, i, (int)row, lo) >> (4 * qd);
-    float pr[4], mx = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      pr[r] = (mw >> r) & 1ull ? score[r] : -INFINITY;
-      mx = fmaxf(mx, pr[r]);
-    }
-    mx = fmaxf(mx, shfl_xor_f(mx, 16));
-    mx = fmaxf(mx, shfl_xor_f(mx, 32));
-    // the reference exponent is an integer: factors between tiles are powers
-    // of two and round nothing
-    const float m_new = fmaxf(m_run, ceilf(mx)), base = m_new == -INFINITY ? 0.f : m_new;
-    if (__any(m_new > m_run)) {
-      const float alpha = exp2f(m_run - base);
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < KS; ++dt) o[dt] *= alpha;
-      m_run = m_new;
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) pr[r] = exp2f(pr[r] - base);
-    l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
-#pragma unroll
-    for (int dt = 0; dt < KS; ++dt) {
-      f32x4 pv[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        pv[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[r][dt >> 2][dt & 3], pr[r], pv[r & 1], 0, 0, 0);
-      o[dt] += pv[0] + pv[1];
-    }
-  }
-  l_run += shfl_xor_f(l_run, 16);
-  l_run += shfl_xor_f(l_run, 32);
-#pragma unroll
-  for (int dt = 0; dt < KS; ++dt) o_s[wave][dt][lane] = o[dt];
-  if (qd == 0) ml_s[wave][c] = f32x2_t{m_run, l_run};
-  f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int dt = 0; dt < KS; ++dt) zero += o[dt] * 0.f;
-  const int odd = __any(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f));
-  if (lane == 0) odd_s[wave] = (odd ? 1 : 0) | (__any(bad) ? 2 : 0);
-  __syncthreads();
-  float m = -INFINITY, den = 0.f;
-  for (int w = 0; w < NW; ++w) m = fmaxf(m, ml_s[w][c][0]);
-  const float base = m == -INFINITY ? 0.f : m;
-  const bool poison = __any(lane < NW && (odd_s[lane < NW ? lane : 0] & 2));
-  // A value of V that is not finite counts only for the query rows that give
-  // its key a weight, but the matrix products multiply it by the zeros of the
-  // others too, and zero times it is NaN.  So where a wave's sums are not
-  // finite the block adds its keys once more, one by one and relative to the
-  // rows' final exponents, without those of weight zero.
-  if (__any(lane < NW && (odd_s[lane < NW ? lane : 0] & 1))) {
-    __syncthreads();  // every wave has read ml_s and odd_s
-    l_run = 0.f;
+      for (int s = 0; s < KS; ++s) kv[s] = load4(kr + 16 * s);
+    };
+    f32x4 o[KS];
 #pragma unroll
     for (int dt = 0; dt < KS; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+    if (s0 + wave < s1) load_k(s0 + wave);
     for (int t = s0 + wave; t < s1; t += NW) {
       const int lo = 16 * t;
-      const long long tb = tile_base(t);
-      const uint64_t mw = seen(p, it, i, (int)row, lo);
-#pragma unroll 1
-      for (int j = 0; j < 16 && lo + j < it.limit; ++j) {
-        const float* kr = kp + tb + (size_t)j * D + 4 * qd;
-        f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
+      f32x4 vv[4][D / 64];
+      const float* const vb = vp + tile_base(t);
 #pragma unroll
-        for (int s = 0; s < KS; ++s) s4 += load4(kr + 16 * s) * (load4(qrow + 16 * s) * a.scale_log2e);
-        float sc = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-        sc += shfl_xor_f(sc, 16);
-        sc += shfl_xor_f(sc, 32);
-        const float pk = (mw >> j) & 1ull ? exp2f(sc - base) : 0.f;
-        if (pk == 0.f) continue;
-        l_run += pk;
-        const float* vr = vp + tb + (size_t)j * D + 16 * qd;
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int h = 0; h < D / 64; ++h)
+          vv[r][h] = load4(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
+      f32x4 score = {0.f, 0.f, 0.f, 0.f};
+      // chains of eight products added in a tree: few roundings in a row
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f32x4 x = load4(vr + 64 * h + 4 * e);
+      for (int s = 0; s < KS; s += 4) {
+        f32x4 sc[8];
 #pragma unroll
-            for (int d4 = 0; d4 < 4; ++d4) o[4 * h + d4][e] += pk * x[d4];
+        for (int ch = 0; ch < 8; ++ch) sc[ch] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int ch = 0; ch < 8; ++ch) {
+            const int x = s + ch / 2, e = 2 * (ch & 1) + j;
+            sc[ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[x][e], qv[x][e], sc[ch], 0, 0, 0);
           }
+        score += ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
+      }
+      if (t + NW < s1) load_k(t + NW);
+      uint64_t mw = ~0ull;
+      if (lo + 16 > all) mw = seen(p, it, i, (int)row, lo) >> (4 * qd);
+      float pr[4], mx = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        pr[r] = (mw >> r) & 1ull ? score[r] : -INFINITY;
+        mx = fmaxf(mx, pr[r]);
+      }
+      mx = fmaxf(mx, shfl_xor_f(mx, 16));
+      mx = fmaxf(mx, shfl_xor_f(mx, 32));
+      // the reference exponent is an integer: factors between tiles are powers
+      // of two and round nothing
+      const float m_new = fmaxf(m_run, ceilf(mx)), base = m_new == -INFINITY ? 0.f : m_new;
+      if (__any(m_new > m_run)) {
+        const float alpha = exp2f(m_run - base);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < KS; ++dt) o[dt] *= alpha;
+        m_run = m_new;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) pr[r] = exp2f(pr[r] - base);
+      l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+#pragma unroll
+      for (int dt = 0; dt < KS; ++dt) {
+        f32x4 pv[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          pv[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[r][dt >> 2][dt & 3], pr[r], pv[r & 1], 0, 0, 0);
+        o[dt] += pv[0] + pv[1];
       }
     }
+    l_run += shfl_xor_f(l_run, 16);
+    l_run += shfl_xor_f(l_run, 32);
 #pragma unroll
     for (int dt = 0; dt < KS; ++dt) o_s[wave][dt][lane] = o[dt];
-    if (qd == 0) ml_s[wave][c] = f32x2_t{m, l_run};
-    __syncthreads();
-  }
-  if (wave >= KS || !on) return;  // wave dt adds accumulator dt
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int w = 0; w < NW; ++w) {
-    const f32x2_t ml = ml_s[w][c];
-    const float wgt = exp2f(ml[0] - base);
-    den += wgt * ml[1];
-    acc += wgt * o_s[w][wave][lane];
-  }
-  if (poison) den = __builtin_nanf("");
-  if (it.flags & kDirect) {
-    const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees no key is zero
-    float* orow = (float*)a.out + (row * p.Hq + head_q) * D + 64 * (wave >> 2) + 16 * qd + (wave & 3);
+    if (qd == 0) ml_s[wave][c] = f32x2_t{m_run, l_run};
+    f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int r = 0; r < 4; ++r) orow[4 * r] = acc[r] * inv;
-  } else if (it.slot < a.max_slots) {
-    const size_t sl = (size_t)it.slot * p.Hkv + g;
-    reinterpret_cast<f32x4*>(a.part_o)[(sl * KS + wave) * 64 + lane] = acc;
-    if (wave == 0 && qd == 0) reinterpret_cast<f32x2_t*>(a.part_ml)[sl * 16 + c] = f32x2_t{m, den};
-  }
+    for (int dt = 0; dt < KS; ++dt) zero += o[dt] * 0.f;
+    const int odd = __any(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f));
+    if (lane == 0) odd_s[wave] = (odd ? 1 : 0) | (__any(bad) ? 2 : 0);
+    __syncthreads();
+    float m = -INFINITY, den = 0.f;
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, ml_s[w][c][0]);
+    const float base = m == -INFINITY ? 0.f : m;
+    const bool poison = __any(lane < NW && (odd_s[lane < NW ? lane : 0] & 2));
+    // A value of V that is not finite counts only for the query rows that give
+    // its key a weight, but the matrix products multiply it by the zeros of the
+    // others too, and zero times it is NaN.  So where a wave's sums are not
+    // finite the block adds its keys once more, one by one and relative to the
+    // rows' final exponents, without those of weight zero.
+    if (__any(lane < NW && (odd_s[lane < NW ? lane : 0] & 1))) {
+      __syncthreads();  // every wave has read ml_s and odd_s
+      l_run = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < KS; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = s0 + wave; t < s1; t += NW) {
+        const int lo = 16 * t;
+        const long long tb = tile_base(t);
+        const uint64_t mw = seen(p, it, i, (int)row, lo);
+#pragma unroll 1
+        for (int j = 0; j < 16 && lo + j < it.limit; ++j) {
+          const float* kr = kp + tb + (size_t)j * D + 4 * qd;
+          f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) s4 += load4(kr + 16 * s) * (load4(qrow + 16 * s) * a.scale_log2e);
+          float sc = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+          sc += shfl_xor_f(sc, 16);
+          sc += shfl_xor_f(sc, 32);
+          const float pk = (mw >> j) & 1ull ? exp2f(sc - base) : 0.f;
+          if (pk == 0.f) continue;
+          l_run += pk;
+          const float* vr = vp + tb + (size_t)j * D + 16 * qd;
+#pragma unroll
+          for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const f32x4 x = load4(vr + 64 * h + 4 * e);
+#pragma unroll
+              for (int d4 = 0; d4 < 4; ++d4) o[4 * h + d4][e] += pk * x[d4];
+            }
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < KS; ++dt) o_s[wave][dt][lane] = o[dt];
+      if (qd == 0) ml_s[wave][c] = f32x2_t{m, l_run};
+      __syncthreads();
+    }
+    if (wave >= KS || !on) return;  // wave dt adds accumulator dt
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int w = 0; w < NW; ++w) {
+      const f32x2_t ml = ml_s[w][c];
+      const float wgt = exp2f(ml[0] - base);
+      den += wgt * ml[1];
+      acc += wgt * o_s[w][wave][lane];
+    }
+    if (poison) den = __builtin_nanf("");
+    if (it.flags & kDirect) {
+      const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees no key is zero
+      float* orow = (float*)a.out + (row * p.Hq + head_q) * D + 64 * (wave >> 2) + 16 * qd + (wave & 3);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) orow[4 * r] = acc[r] * inv;
+    } else if (it.slot < a.max_slots) {
+      const size_t sl = (size_t)it.slot * p.Hkv + g;
+      reinterpret_cast<f32x4*>(a.part_o)[(sl * KS + wave) * 64 + lane] = acc;
+      if (wave == 0 && qd == 0) reinterpret_cast<f32x2_t*>(a.part_ml)[sl * 16 + c] = f32x2_t{m, den};
+    }
+  });
 }
 
 // ------------------------------------------------------------------- join
@@ -448,18 +570,19 @@ __global__ __launch_bounds__(64) void join_kernel(PagedAttnArgs a) {
     if (wb > 0.f) acc += o * wb;  // zero times an infinite sum is not zero
     m = mn;
   };
-  const int sb = head.shared_block, sg = sb / GR;
-  for (int s = 0; s < head.shared_splits; ++s)
-    add(head.shared_slot0 + ((long long)(x / sb) * head.shared_splits + s) * sg + (x % sb) / GR, c);
+  if (const int sb = head.shared_block) {
+    const BlockSlots d = reinterpret_cast<const BlockSlots*>(a.plan + a.off_blocks)[x / sb];
+    for (int s = 0; s < d.splits; ++s) add(d.slot + (long long)s * d.groups + (x % sb) / GR, c);
+  }
   for (int s = 0; s < rs.splits; ++s) add(rs.slot + (long long)s * rs.stride, rs.row);
   put(acc * (den == 0.f ? 0.f : 1.f / den));
 }
 
 template <class T, int D>
 void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
-  const unsigned items = (unsigned)(s.max_items * a.p.Hkv);
+  const unsigned items = (unsigned)(s.workers * a.p.Hkv);
   if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
-  else paged_attn_f32_kernel<D><<<items, 64 * 1024 / D, 0, st>>>(a);
+  else paged_attn_f32_kernel<D><<<items, 512, 0, st>>>(a);
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
   join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D * s.group / 256)), 64, 0, st>>>(a);
 }
@@ -492,7 +615,7 @@ extern "C" int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t p
   PlanHead head{};
   plan_key(*batch, head.key);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  plan_kernel<<<1, kPlanThreads, 0, st>>>(p, s, head, (uint8_t*)plan);
+  plan_kernel<<<1, kPlanThreads, 0, st>>>(p, s, head, batch->head_dim == 64, (uint8_t*)plan);
   const long long q = (long long)p.n_rows * p.G;
   plan_rows_kernel<<<(unsigned)((q + 255) / 256), 256, 0, st>>>(p, s, (uint8_t*)plan);
   const hipError_t e = hipGetLastError();
@@ -525,8 +648,15 @@ extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, si
               ws_bytes);
   plan_key(*batch, a.want.key);
   a.plan = (const uint8_t*)plan;
-  a.off_items = s.off_items;
+  a.off_blocks = s.off_blocks;
+  a.off_first_w = s.off_first_w;
+  a.off_first_n = s.off_first_n;
+  a.off_items_w = s.off_items_w;
+  a.off_items_n = s.off_items_n;
   a.off_rows = s.off_rows;
+  a.max_items_w = (int)s.max_items_w;
+  a.max_items_n = (int)s.max_items_n;
+  a.workers = s.workers;
   a.q = q;
   a.k = k_pages;
   a.v = v_pages;

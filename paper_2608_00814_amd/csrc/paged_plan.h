@@ -7,14 +7,27 @@
 //   own blocks     up to `wide` consecutive query rows of one sequence (one
 //                  block of up to `narrow` where there are few), against the
 //                  sequence's own tokens;
-//   shared blocks  up to `wide` query rows of the whole stack, against the
-//                  shared prompt, which is so read once for many sequences.
-// A block's keys go in tiles of 64, and its tiles are split evenly into
-// *items*, one workgroup per KV head each, so that all items cost about the
-// same: total cost / `target`.  An item leaves unnormalised sums and softmax
-// statistics in *slots* of `group` query rows; a second kernel joins the slots
-// of every row.  A block with one item and no shared part writes its output
-// itself.
+//   shared blocks  the same of the whole stack, against the shared prompt,
+//                  which is so read once for many sequences.
+// A KV head's work goes to `workers` workgroups, all on the chip at once:
+//  * the first ones take the wide shared blocks, each cut into the same number
+//    of runs of its tiles of 64 keys.  A run of a block is an *item*; the items
+//    are dealt out with the block index moving fastest, so that workgroups
+//    that run at the same time read the same part of the prompt and share it
+//    in their XCD's L2.  (Cut into equal runs one block behind the other, the
+//    balance is perfect, but each workgroup is in another place of the prompt:
+//    eight tries of 64 over a 4k prompt took 69 us so, 53 dealt out like this.)
+//  * the next take the sequences' own wide blocks, one behind the other, in
+//    runs of equal cost: a block's tiles and, ahead of them, as many as the
+//    start and end of an item cost (runs of equal length left four prompts of
+//    300 to 512 rows with workgroups 13 us behind the others);
+//  * the last take the narrow blocks' half-tiles of 32 keys in the same way, a
+//    run for each of their waves.
+// The numbers of workgroups and runs are those that finish first by the costs
+// in paged_attn.hip.  The part of a block in one run leaves unnormalised sums and softmax
+// statistics in *slots* of `group` query rows, and a second kernel joins the
+// slots of every row.  A block of one item and without a shared part writes
+// its output itself.
 #pragma once
 
 #include "paged.h"
@@ -22,22 +35,23 @@
 namespace ooo {
 
 constexpr int kTileKeys = 64;
+constexpr int kSplitMost = 4;  // extra items of the shared blocks: at most so many times the workers
 
 struct PlanShape {
-  int narrow, wide, group;         // query rows
-  int cost_narrow, cost_wide;      // of a tile
-  int target;                      // items of a KV head aimed at
-  long long max_blocks, max_items, max_slots;
-  long long off_blocks, off_seqs, off_items, off_rows, bytes;
+  int narrow, wide, group;  // query rows (narrow 0: there are no narrow blocks)
+  int waves;                // of a worker, where narrow blocks are one wave's work
+  int workers;              // workgroups of a KV head
+  long long max_blocks, max_items_w, max_items_n, max_slots;
+  long long off_blocks, off_seqs, off_first_w, off_first_n, off_items_w, off_items_n, off_rows, bytes;
 };
 
 // Item record (16 ints).
 struct Item {
-  int flags;   // kShared | kWide | kDirect
+  int flags;   // kShared | kDirect
   int seq;
   int row0;    // the sequence's first row (0 for shared blocks)
   int q0, nq;  // query rows [q0, q0 + nq) of the sequence or of the stack
-  int t0, t1;  // tiles
+  int t0, t1;  // tiles (wide) or half-tiles (narrow)
   int limit;   // keys of the block (those from limit on are not read)
   int len;     // own committed tokens (shared: the limit)
   int rows;    // the sequence's new rows
@@ -45,20 +59,25 @@ struct Item {
   int pad[5];
 };
 static_assert(sizeof(Item) == 64, "item record");
-enum { kShared = 1, kWide = 2, kDirect = 4 };
+enum { kShared = 1, kDirect = 4 };
 
 // Head of the plan.
 struct PlanHead {
   int key[8];       // the sizes it was made for
-  int items;
   int rows;         // new rows there are
-  int shared_splits, shared_block, shared_slot0;
-  int pad[3];
+  int shared_block; // query rows of a shared block (0: no shared part)
+  int shared_items, shared_workers;              // wide ones
+  int own_first, own_workers;                    // workers with own wide runs
+  int narrow_first, narrow_workers;
 };
 static_assert(sizeof(PlanHead) == 64, "plan head");
 
-// Slots of one query row in its own part; the shared part follows from the
-// head.  splits 0: the row is written by its item.
+// Slots of one block: `splits` times `groups` of them, from `slot` on.
+// splits 0: written by its item.
+struct BlockSlots {
+  int slot, splits, groups, pad;
+};
+// Slots of one query row in its own part.
 struct RowSlots {
   int slot, splits, stride, row;
 };
@@ -67,22 +86,27 @@ inline PlanShape plan_shape(const ooo_paged_batch& b) {
   PlanShape s{};
   const bool bf = b.dt == OOO_BF16;
   s.group = bf ? 32 : 16;
-  s.narrow = s.group;
+  s.narrow = bf ? 32 : 0;
   s.wide = bf ? 128 : 16;
-  s.cost_narrow = s.cost_wide = 1;
-  s.target = (bf ? 1 : 2) * device_cus() / b.n_kv_heads;
-  if (s.target < 1) s.target = 1;
+  s.waves = bf ? 8 : 0;
+  s.workers = (bf ? 1 : 2) * device_cus() / b.n_kv_heads;
+  if (s.workers < 1) s.workers = 1;
   const long long G = b.n_q_heads / b.n_kv_heads, q = b.n_rows * G;
-  const long long stack = b.shared_len > 0 ? (q + s.group - 1) / s.group : 0;
-  // a sequence's last block may be short, so one more than the full ones each
-  s.max_blocks = b.n_seqs + q / s.wide;
-  s.max_items = s.max_blocks + stack + s.target;
-  s.max_slots = b.n_seqs + q / s.group + stack + (long long)(s.wide / s.group) * (s.target + (stack > 0));
+  const long long shared = b.shared_len > 0 ? (q + s.wide - 1) / s.wide : 0;
+  const long long own = b.n_seqs + q / s.wide;  // a sequence's last block may be short
+  s.max_blocks = shared + own;
+  s.max_items_w = s.max_blocks + (kSplitMost + 1ll) * s.workers;
+  s.max_items_n = bf ? b.n_seqs + 1 + (long long)s.waves * s.workers : 0;
+  const long long per_wide = s.wide / s.group, runs = s.workers * (per_wide + s.waves);
+  s.max_slots = b.n_seqs + 1 + q / s.group + (shared + (long long)kSplitMost * s.workers) * per_wide + runs;
   const auto up = [](long long n) { return (n + 63) / 64 * 64; };
   s.off_blocks = sizeof(PlanHead);
-  s.off_seqs = up(s.off_blocks + s.max_blocks * 16);
-  s.off_items = up(s.off_seqs + (b.n_seqs + 1) * 4ll);
-  s.off_rows = s.off_items + s.max_items * (long long)sizeof(Item);
+  s.off_seqs = up(s.off_blocks + s.max_blocks * (long long)sizeof(BlockSlots));
+  s.off_first_w = up(s.off_seqs + (b.n_seqs + 1) * 4ll);
+  s.off_first_n = up(s.off_first_w + (s.workers + 1) * 4ll);
+  s.off_items_w = up(s.off_first_n + (s.waves * s.workers + 1) * 4ll);
+  s.off_items_n = s.off_items_w + s.max_items_w * (long long)sizeof(Item);
+  s.off_rows = s.off_items_n + s.max_items_n * (long long)sizeof(Item);
   s.bytes = s.off_rows + q * (long long)sizeof(RowSlots);
   return s;
 }
@@ -90,7 +114,7 @@ inline PlanShape plan_shape(const ooo_paged_batch& b) {
 // Whether the workgroups of the largest plan can be launched.
 inline bool plan_grid_ok(const ooo_paged_batch& b, const PlanShape& s) {
   const double join = ((double)b.n_rows * (b.n_q_heads / b.n_kv_heads) / s.group + 1) * b.n_kv_heads * b.head_dim;
-  return (double)s.max_items * b.n_kv_heads <= 1073741824.0 && join <= 1073741824.0;
+  return (double)s.workers * b.n_kv_heads <= 1073741824.0 && join <= 1073741824.0;
 }
 
 // The sizes that a plan belongs to.

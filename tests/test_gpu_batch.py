@@ -227,6 +227,19 @@ def test_attn_bounds_device_values():
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attn_same_bits_every_time(dt, D):
+    """Short and long items of both kinds, with other work in between."""
+    other = torch.empty(1 << 26, device="cuda")
+    for rows, lens, shared in (([2, 1, 3], [40, 50, 20], 20), ([1] * 9, [700] * 9, 0), ([90, 1, 33], [500, 90, 7], 300)):
+        b = Batch(dt, 4, 2, D, 16, rows, lens, shared=shared)
+        first = b.attend()
+        for _ in range(6):
+            other.fill_(float("nan"))
+            assert torch.equal(b.attend(), first)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_attn_deterministic_and_on_a_stream(dt):
     b = Batch(dt, 8, 2, 128, 32, [1, 5, 40], [500, 90, 7], shared=300)
     a = b.attend()
