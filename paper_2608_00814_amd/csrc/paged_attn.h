@@ -10,7 +10,7 @@ struct PagedAttnArgs {
   Paged p;
   PlanHead want;        // key to compare with
   const uint8_t* plan;
-  long long off_blocks, off_first_w, off_first_n, off_items_w, off_items_n, off_rows;
+  long long off_first_w, off_first_n, off_items_w, off_items_n, off_rows;
   int max_items_w, max_items_n, workers;
   const void* q;
   const void* k;

@@ -316,15 +316,19 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, ui
   }
   const Seq q = seq_of(p, lo, R);
   const int rows = q.rows * p.G, at = x - q.row0 * p.G;
-  RowSlots o{0, 0, 0, 0};
+  RowSlots o{};
   if (at >= 0 && at < rows) {
     const int block = rows > s.narrow ? s.wide : s.narrow;
     const long long blk = reinterpret_cast<const int*>(plan + s.off_seqs)[lo] + at / block;
     if (blk < s.max_blocks) {
       const BlockSlots d = reinterpret_cast<const BlockSlots*>(plan + s.off_blocks)[blk];
       const int in = at % block;
-      o = RowSlots{d.slot + in / s.group, d.splits, d.groups, in % s.group};
+      o.part[1] = {d.slot + in / s.group, d.splits, d.groups, in % s.group};
     }
+  }
+  if (const int sb = reinterpret_cast<const PlanHead*>(plan)->shared_block) {
+    const BlockSlots d = reinterpret_cast<const BlockSlots*>(plan + s.off_blocks)[x / sb];
+    o.part[0] = {d.slot + x % sb / s.group, d.splits, d.groups, x % s.group};
   }
   reinterpret_cast<RowSlots*>(plan + s.off_rows)[x] = o;
 }
@@ -523,23 +527,26 @@ __global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
 }
 
 // ------------------------------------------------------------------- join
-// One wave per (group of stacked query rows, KV head, accumulator piece): a
-// lane joins 4 columns of one row over the row's shared and own slots.  Lane
-// (c, q) of a piece holds row c and, in float32 (groups of 16), columns 64
-// (piece / 4) + 16 q + 4 e + piece % 4; in bf16 (groups of 32) columns
-// 8 piece + 4 q + e.
+// Adds the parts of every row: 4 waves, one for each of 4 accumulator pieces of
+// a group of stacked query rows and KV head; a lane joins 4 columns of one row
+// over the row's shared and own slots.  Lane (c, q) of a piece holds row c and,
+// in float32 (groups of 16), columns 64 (piece / 4) + 16 q + 4 e + piece % 4;
+// in bf16 (groups of 32) columns 8 piece + 4 q + e.  Bound by latency: the
+// plan's head and the row's slots are asked for together, then four slots at a
+// time.
 template <class T, int D>
-__global__ __launch_bounds__(64) void join_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int GR = BF ? 32 : 16, NP = D * GR / 256;
+  constexpr int AT_ONCE = 4;
   const Paged& p = a.p;
-  const PlanHead head = load_head(a);
-  const int lane = threadIdx.x, c = lane % GR, qd = lane / GR;
-  int w = blockIdx.x;
-  const int pc = w % NP;
-  w /= NP;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane % GR, qd = lane / GR;
+  const int w = blockIdx.x / (NP / 4), pc = 4 * (blockIdx.x % (NP / 4)) + wave;
   const int g = w % p.Hkv, x = (w / p.Hkv) * GR + c;
   const int i = x / p.G, h = g * p.G + x - i * p.G;
+  const PlanHead head = load_head(a);
+  const RowSlots rs = reinterpret_cast<const RowSlots*>(a.plan + a.off_rows)[min(x, p.n_rows * p.G - 1)];
   const bool fits = plan_fits(head, a.want);
   if (i >= (fits ? head.rows : min(p.row_start[p.n_seqs], p.n_rows))) return;
   T* const orow = (T*)a.out + ((size_t)i * p.Hq + h) * D;
@@ -555,26 +562,37 @@ __global__ __launch_bounds__(64) void join_kernel(PagedAttnArgs a) {
     put(f32x4{nan, nan, nan, nan});
     return;
   }
-  const RowSlots rs = reinterpret_cast<const RowSlots*>(a.plan + a.off_rows)[x];
-  if (rs.splits == 0) return;  // written by its item
+  const int n0 = rs.part[0].splits, n = n0 + rs.part[1].splits;
+  if (rs.part[1].splits == 0) return;  // written by its item
   float m = -INFINITY, den = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  const auto add = [&](long long slot, int rw) {
-    const size_t sl = (size_t)min(slot, a.max_slots - 1) * p.Hkv + g;
-    const f32x2_t ml = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * GR + rw];
-    const f32x4 o = reinterpret_cast<const f32x4*>(a.part_o)[(sl * NP + pc) * 64 + GR * qd + rw];
-    const float mn = fmaxf(m, ml[0]), base = mn == -INFINITY ? 0.f : mn;
-    const float wa = exp2f(m - base), wb = exp2f(ml[0] - base);
-    den = den * wa + ml[1] * wb;
-    acc = acc * wa;
-    if (wb > 0.f) acc += o * wb;  // zero times an infinite sum is not zero
+  for (int s = 0; s < n; s += AT_ONCE) {
+    f32x2_t ml[AT_ONCE];
+    f32x4 o[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {  // past the last one: that again
+      const int t = min(s + k, n - 1);
+      const RowSlots::Part& r = rs.part[t < n0 ? 0 : 1];
+      const long long slot = r.slot + (long long)(t < n0 ? t : t - n0) * r.stride;
+      const size_t sl = (size_t)min(slot, a.max_slots - 1) * p.Hkv + g;
+      ml[k] = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * GR + r.row];
+      o[k] = reinterpret_cast<const f32x4*>(a.part_o)[(sl * NP + pc) * 64 + GR * qd + r.row];
+    }
+    float mn = m;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) mn = fmaxf(mn, ml[k][0]);
+    const float base = mn == -INFINITY ? 0.f : mn;
+    const float wa = exp2f(m - base);
+    den *= wa;
+    acc *= wa;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const float wb = s + k < n ? exp2f(ml[k][0] - base) : 0.f;
+      if (s + k < n) den += ml[k][1] * wb;
+      if (wb > 0.f) acc += o[k] * wb;  // zero times an infinite sum is not zero
+    }
     m = mn;
-  };
-  if (const int sb = head.shared_block) {
-    const BlockSlots d = reinterpret_cast<const BlockSlots*>(a.plan + a.off_blocks)[x / sb];
-    for (int s = 0; s < d.splits; ++s) add(d.slot + (long long)s * d.groups + (x % sb) / GR, c);
   }
-  for (int s = 0; s < rs.splits; ++s) add(rs.slot + (long long)s * rs.stride, rs.row);
   put(acc * (den == 0.f ? 0.f : 1.f / den));
 }
 
@@ -584,7 +602,7 @@ void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
   if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
   else paged_attn_f32_kernel<D><<<items, 512, 0, st>>>(a);
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
-  join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D * s.group / 256)), 64, 0, st>>>(a);
+  join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D * s.group / 1024)), 256, 0, st>>>(a);
 }
 
 size_t workspace_bytes(const ooo_paged_batch& b, const PlanShape& s) {
@@ -648,7 +666,6 @@ extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, si
               ws_bytes);
   plan_key(*batch, a.want.key);
   a.plan = (const uint8_t*)plan;
-  a.off_blocks = s.off_blocks;
   a.off_first_w = s.off_first_w;
   a.off_first_n = s.off_first_n;
   a.off_items_w = s.off_items_w;

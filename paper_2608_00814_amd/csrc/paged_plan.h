@@ -77,9 +77,11 @@ static_assert(sizeof(PlanHead) == 64, "plan head");
 struct BlockSlots {
   int slot, splits, groups, pad;
 };
-// Slots of one query row in its own part.
+// Slots of one query row: in the shared part and in its own.
 struct RowSlots {
-  int slot, splits, stride, row;
+  struct Part {
+    int slot, splits, stride, row;  // splits 0: none, or written by its item
+  } part[2];
 };
 
 inline PlanShape plan_shape(const ooo_paged_batch& b) {
