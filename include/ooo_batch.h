@@ -47,8 +47,9 @@ extern "C" {
  * row_start[b] .. row_start[b + 1] - 1 of q, qkv and out (none is allowed).
  * Rows from row_start[n_seqs] to n_rows are never touched.
  *
- *   n_seqs        sequences (1 .. 65536)
- *   n_rows        rows the step's buffers hold; row_start[n_seqs] <= n_rows
+ *   n_seqs        sequences (1 .. 65535)
+ *   n_rows        rows the step's buffers hold; row_start[n_seqs] <= n_rows;
+ *                 n_rows * n_q_heads and n_rows * mask_words up to 2^28
  *   row_start     [n_seqs + 1] int32, non-decreasing, row_start[0] == 0
  *   seq_len       [n_seqs] int32, >= 0
  *   page_table    [n_seqs][table_ld] int32
@@ -170,7 +171,8 @@ int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_b
  *   accept_len    [n_seqs] int32; -1, or a length that path_cap does not
  *                 hold, moves no row of that sequence
  * Entries of path outside the sequence's new rows, and rows whose place is
- * past the page table or in a page outside [0, n_pages), are not moved.
+ * past the page table or in a page outside [0, n_pages), are not moved.  No
+ * two sequences' new rows may lie in one place (as for ooo_paged_append).
  * Errors: as for ooo_paged_append; OOO_ERR_INVALID (n_layers or path_cap < 1).
  */
 int ooo_paged_compact(const ooo_paged_batch* batch, void* k_pages, void* v_pages, int32_t n_layers,

@@ -40,12 +40,14 @@ inline int check_paged(const char* who, const ooo_paged_batch* b, Paged& p) {
               "%s: head_dim %d not supported (64 or 128)", who, b->head_dim);
   OOO_REQUIRE(b->page_rows >= 16 && b->page_rows <= 65536 && (b->page_rows & (b->page_rows - 1)) == 0,
               OOO_ERR_UNSUPPORTED, "%s: page_rows %d not supported (a power of two, 16 to 65536)", who, b->page_rows);
-  OOO_REQUIRE(b->n_seqs <= 65536, OOO_ERR_UNSUPPORTED, "%s: n_seqs %d above 65536", who, b->n_seqs);
+  OOO_REQUIRE(b->n_seqs <= 65535, OOO_ERR_UNSUPPORTED, "%s: n_seqs %d above 65535", who, b->n_seqs);
   const int64_t own = (int64_t)b->table_ld * b->page_rows;
   OOO_REQUIRE(own <= (1 << 30) && b->shared_len <= (1 << 30), OOO_ERR_UNSUPPORTED,
               "%s: more than 2^30 tokens a sequence", who);
   OOO_REQUIRE((int64_t)b->n_rows * b->n_q_heads <= (1 << 28), OOO_ERR_UNSUPPORTED,
               "%s: n_rows * n_q_heads above 2^28", who);
+  OOO_REQUIRE((int64_t)b->n_rows * b->mask_words <= (1 << 28), OOO_ERR_UNSUPPORTED,
+              "%s: n_rows * mask_words above 2^28", who);  // kernels use 32-bit offsets into the mask
   const int64_t page = (int64_t)b->n_kv_heads * b->page_rows * b->head_dim;
   OOO_REQUIRE(b->page_stride >= page, OOO_ERR_INVALID, "%s: page_stride %lld below a page's %lld elements", who,
               (long long)b->page_stride, (long long)page);

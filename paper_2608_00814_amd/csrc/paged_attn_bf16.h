@@ -339,7 +339,7 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
     barrier(0);
     if (idle) {  // copies and keeps step
 #pragma unroll 1
-      for (int m = 1; m <= tiles; ++m) {
+      for (int m = 1; m <= tiles + 1; ++m) {
         ask_v(m, 1);
         ask_k(m + 2);
         barrier(m);
@@ -374,7 +374,7 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             wait_vmcnt<2 * PM>();
             wg_barrier();
-          } else if (n + 2 <= tiles) {
+          } else {
             barrier(n + 2);
           }
         };

@@ -221,7 +221,6 @@ extern "C" int ooo_paged_compact(const ooo_paged_batch* batch, void* k_pages, vo
   OOO_REQUIRE(n_layers >= 1 && path_cap >= 1, OOO_ERR_INVALID, "ooo_paged_compact: n_layers and path_cap must be >= 1");
   OOO_REQUIRE(n_layers == 1 || layer_stride >= 1, OOO_ERR_INVALID, "ooo_paged_compact: layer_stride must be >= 1");
   OOO_REQUIRE(n_layers <= 65535, OOO_ERR_UNSUPPORTED, "ooo_paged_compact: n_layers %d above 65535", n_layers);
-  OOO_REQUIRE(p.n_seqs <= 65535, OOO_ERR_UNSUPPORTED, "ooo_paged_compact: n_seqs %d above 65535", p.n_seqs);
   const int elt = batch->dt == OOO_BF16 ? 2 : 4;
   OOO_REQUIRE(layer_stride * elt % 16 == 0 && aligned16(k_pages) && aligned16(v_pages), OOO_ERR_UNSUPPORTED,
               "ooo_paged_compact: a pointer or layer_stride is not a multiple of 16 bytes");

@@ -69,6 +69,20 @@ def test_bad_batches(kw, status):
     assert ooo.lib().ooo_paged_attn_workspace(ctypes.addressof(b)) == 0
 
 
+@pytest.mark.parametrize("kw", [dict(n_seqs=65536),
+                                dict(anc_mask=P, mask_words=16, n_rows=1 << 25, n_q_heads=8, n_kv_heads=8)])
+def test_sizes_past_the_kernels_offsets(kw):
+    for rc in calls(struct(**kw)):
+        assert rc == ooo.ERR_UNSUPPORTED, ooo.last_error()
+
+
+def test_sample_rows_and_alignment():
+    L = ooo.lib()
+    s = lambda n=4, w=P: L.ooo_sample(P, 1000, ooo.F32, n, 1000, None, None, None, None, P, P, None, None, w,  # noqa: E731
+                                      1 << 40, None)
+    assert s(n=65536) == s(w=P + 8) == ooo.ERR_UNSUPPORTED
+
+
 def test_null_batch():
     L = ooo.lib()
     assert L.ooo_paged_plan(None, P, 64, None) == ooo.ERR_INVALID

@@ -272,6 +272,57 @@ def test_attn_pool_past_32_bits():
     assert torch.equal(b.attend(), want)
 
 
+@pytest.mark.parametrize("dt,shared", [("bf16", 0), ("bf16", 70), ("f32", 33)])
+def test_attn_many_sequences(dt, shared):
+    r = random.Random(5)
+    lens = ragged(r, 700, 20)
+    b = Batch(dt, 4, 2, 64, 16, [1] * 699 + [35], lens, shared=shared, pad=1, seed=1)
+    b.check(b.attend())
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("shared", [0, 2601, 4096])
+def test_attn_many_pages(dt, D, shared):
+    """Hundreds of the smallest pages to a part, in both kinds of it."""
+    for rows, lens in (([1, 2], [5003, 3]), ([70, 1], [2100, 4100])):
+        b = Batch(dt, 2, 1, D, 16, rows, lens, shared=shared, seed=shared)
+        b.check(b.attend())
+
+
+@pytest.mark.parametrize("dt,heads", [("bf16", 100), ("bf16", 256), ("f32", 300)])
+def test_attn_more_heads_than_work_is_shared_over(dt, heads):
+    for shared in (0, 50):
+        b = Batch(dt, heads, heads, 64, 16, [1, 40, 2], [30, 70, 5], shared=shared, pad=1, seed=heads)
+        b.check(b.attend())
+
+
+def test_attn_two_batches_on_two_streams():
+    """Captured together and replayed, each with its own plan and workspace."""
+    bs = [Batch("bf16", 8, 2, 128, 16, rows, lens, shared=sh, seed=sh)
+          for rows, lens, sh in (([1] * 6, [900, 40, 300, 0, 64, 5], 500), ([40, 3], [700, 90], 65))]
+    want = [b.attend() for b in bs]
+    keep = [(ooo.paged_plan(b.batch), torch.empty(ooo.paged_attn_workspace(b.batch), dtype=torch.uint8, device="cuda"),
+             torch.empty_like(b.q)) for b in bs]
+    torch.cuda.synchronize()
+    graphs, streams = [], [torch.cuda.Stream() for _ in bs]
+    for b, (plan, ws, out), s in zip(bs, keep, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            ooo.paged_plan(b.batch, plan)
+            ooo.paged_attn(b.batch, plan, b.q, b.k, b.v, b.scale, out, ws)
+        graphs.append(g)
+    for _ in range(4):
+        for _, _, out in keep:
+            out.fill_(7.0)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for (_, _, out), w in zip(keep, want):
+            assert torch.equal(out, w)
+
+
 # ----------------------------------------------------------------- compact
 
 
