@@ -141,8 +141,9 @@ __device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int
   return best;
 }
 
-// One workgroup, 15 us for up to 256 sequences, once a step.  First the lengths, from them the deal, then the items and
-// slots of every entry behind those of the entries before it.
+// One workgroup, 15 us for up to 256 sequences, once a step.  First the
+// lengths, from them the deal, then the items and slots of every entry behind
+// those of the entries before it.
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, int half_dim,
                                                             uint8_t* plan) {
   BlockSlots* const blocks = reinterpret_cast<BlockSlots*>(plan + s.off_blocks);
