@@ -134,6 +134,18 @@ struct Tokens {
     for (int k = 0; k < kAhead; ++k) d[k] = raw4(x, min(at + 4 * NT * k, to), to);
   }
   template <class F>
+  __device__ __forceinline__ void places(F f) {  // f(place in the thread's turn, logit)
+    for (;;) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(4 * k + e, value(v[k][e]));
+      i += 4 * NT * kAhead;
+      if (i - 4 * (int)threadIdx.x >= to) break;
+      load(v, i);
+    }
+  }
+  template <class F>
   __device__ __forceinline__ void each(F f) {  // f(token, logit, NaN and -0 as they are)
     for (; i < to; i += 4 * NT * kAhead) {
       typename Raw<T>::vec next[kAhead];
@@ -163,7 +175,7 @@ constexpr float kLeast = -0x1.fffffep127f;  // the least finite logit
 struct Row {
   float M;             // largest logit, 0 for a row with infinite ones
   bool inf;
-  double c, T;         // log2(e) / T, T
+  double c;            // log2(e) / T
   double floor_y;      // log2(min_p) (-inf: no floor)
   double top_p, u;
   int k, shift;
@@ -182,7 +194,7 @@ struct Row {
   // degree 8 through its values at the Chebyshev nodes (off by 1.1e-12 at
   // most, exact at 0); adding 2^52 rounds to nearest and leaves the number in
   // the low bits.
-  __device__ __forceinline__ u64 weight(double y) const {
+  static __device__ __forceinline__ double exp2_of(double y, int up) {  // 2^(y + up)
     const double n = rint(y), t = y - n;
     double q = 1.3255224878668817e-06;
     q = fma(q, t, 1.5310079402249296e-05);
@@ -193,8 +205,10 @@ struct Row {
     q = fma(q, t, 0.2402265069581299);
     q = fma(q, t, 0.6931471805459335);
     q = fma(q, t, 1.0);
-    const double r = ldexp(q, (int)n + shift) + 0x1p52;
-    return (u64)__double_as_longlong(r) & 0x000FFFFFFFFFFFFFull;
+    return ldexp(q, (int)n + up);
+  }
+  __device__ __forceinline__ u64 weight(double y) const {
+    return (u64)__double_as_longlong(exp2_of(y, shift) + 0x1p52) & 0x000FFFFFFFFFFFFFull;
   }
   __device__ __forceinline__ u64 weight_of(float x) const {
     const double v = y(x);
@@ -224,8 +238,7 @@ struct Settings {
 __device__ __forceinline__ Row row_of(const SampleArgs& a, const Settings& set) {
   Row s;
   const bool greedy = !(set.t > 0.f);
-  s.T = greedy ? 1.0 : (double)set.t;
-  s.c = 1.4426950408889634 / s.T;
+  s.c = 1.4426950408889634 / (greedy ? 1.0 : (double)set.t);
   s.k = greedy ? 1 : set.k > 0 ? set.k : a.vocab;
   s.top_p = set.top_p < 1.f ? fmax((double)set.top_p, 0.0) : set.top_p >= 1.f ? 1.0 : 0.0;
   s.floor_y = set.min_p > 0.f ? log2((double)set.min_p) : -INFINITY;
@@ -237,7 +250,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, const Settings& set) 
 __device__ __forceinline__ void Row::set_max(float largest) {
   inf = largest == INFINITY;
   M = inf ? 0.f : largest;
-  if (inf) T = 1.0, c = 1.4426950408889634;
+  if (inf) c = 1.4426950408889634;
   least = k == 1 ? largest : kLeast;
   if (floor_bin < kLast && top_p >= 1.0 && !inf) least = fmaxf(least, fminf(edge(floor_bin), M));
 }
@@ -618,8 +631,7 @@ __device__ __forceinline__ float logit_of(u64 cand) { return of_key((uint32_t)(c
 __device__ __forceinline__ void write_answer(const SampleArgs& a, int r, const Row& s, int id, float best, u64 n, u64 W) {
   if (threadIdx.x != 0) return;
   a.ids[r] = id;
-  const double z = ((double)best - (double)s.M) / s.T;
-  if (a.prob) a.prob[r] = (float)(exp(z) / ldexp((double)W, -s.shift));
+  if (a.prob) a.prob[r] = (float)(Row::exp2_of(s.y(best), s.shift) / (double)W);
   if (a.kept) a.kept[r] = (int32_t)n;
 }
 
@@ -860,7 +872,7 @@ __device__ __forceinline__ float kth_bound(const float (&v)[PV], const Spread& o
 }
 
 // Tokens that reach `least` are added to m.w as they are found: a thread looks
-// through 32 tokens, then takes places for all it keeps at once.
+// through its turn of tokens, then takes places for all it keeps at once.
 struct Keep {
   uint32_t* n;
   u64* w;
@@ -919,22 +931,29 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a) {
   const Settings set(a, r);
   Tokens<T, NT> first(x, 0, V), again = first, last = first;  // the first turn is loaded once
   Row s = row_of(a, set);
-  float group[1] = {-INFINITY};  // the thread's tokens are a group
-  first.each([&](int, float v) { group[0] = fmaxf(group[0], v); });  // of a number and NaN the number
+  // The tokens in one place of the turns are a group: each token its own up to
+  // 4096 of them, and top-k's bound leaves hardly more than k.
+  constexpr int PV = 4 * kAhead;
+  float group[PV];
+#pragma unroll
+  for (int e = 0; e < PV; ++e) group[e] = -INFINITY;
+  first.places([&](int e, float v) { group[e] = fmaxf(group[e], v); });  // of a number and NaN the number
   if (threadIdx.x == 0) n_cand = over = 0;
-  const Spread of = spread_of<NT, 1>(group);
+  const Spread of = spread_of<NT, PV>(group);
   if (empty_row(a, r, of.M)) return;
   s.set_max(of.M);
   // Few tokens, or top-k by the groups.
-  if (V <= NT || (uint32_t)s.k <= of.n) {
-    const float bound = V <= NT ? kLeast : kth_bound<NT, 1>(group, of, s.k);
+  if (V <= NT || (uint32_t)s.k <= min(of.n, (uint32_t)kFlatK)) {
+    const float bound = V <= NT ? kLeast : kth_bound<NT, PV>(group, of, s.k);
     const Keep keep{&n_cand, h.flat.w, bound};
-    for (; again.i < V; again.i += 4 * NT * kAhead) {
+    for (int i0 = 0;;) {
       int at[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) at[k] = again.i + 4 * NT * k;
       keep(s, again.v, at);
-      again.load(again.v, again.i + 4 * NT * kAhead);
+      again.i += 4 * NT * kAhead;
+      if ((i0 += 4 * NT * kAhead) >= V) break;
+      again.load(again.v, again.i);
     }
     __syncthreads();
     if (n_cand <= kFlat) {
