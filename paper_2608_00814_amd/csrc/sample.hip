@@ -35,9 +35,10 @@
 // 256 rows of 152064 float32 logits take 120 us: the largest logits 26 (HBM, 6
 // TB/s), the histogram 37 (the exponential and LDS atomics) and the gathering 32
 // (the search for the bins in every workgroup) of the third of the rows that
-// have no top-k, the answers 23, one workgroup a row.  A row of 1024 tokens
-// takes 14 us and the answer of a long one with top-k the same: some fifteen
-// barriers, and instructions that run once each and are waited for.
+// have no top-k, the answers 23, one workgroup a row.  Rows of 1024 tokens
+// take 12 us and the answer of a long one with top-k 14: some fifteen barriers,
+// and instructions that run once each and are waited for (the search for the
+// bins 8400 cycles, the ordering of 200 tokens 6100, the histogram 2600).
 #include "device_common.h"
 #include "ooo_batch.h"
 #include "ooo_internal.h"
