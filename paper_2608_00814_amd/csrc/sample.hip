@@ -333,30 +333,57 @@ __device__ __forceinline__ u64 wave_scan(u64 v) {
   v += from_lane<0x143, 0xC>(v);  // lane 31, into rows 2 and 3
   return v;
 }
-// inclusive scan of N values over the threads; the totals go to all
-template <int NT, int N>
-__device__ __forceinline__ void block_scan(u64 (&v)[N], u64 (&total)[N]) {
-  __shared__ u64 sh[N][NT / 64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_u(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += lane_u<0x111, 0xF>(v);
+  v += lane_u<0x112, 0xF>(v);
+  v += lane_u<0x114, 0xF>(v);
+  v += lane_u<0x118, 0xF>(v);
+  v += lane_u<0x142, 0xA>(v);
+  v += lane_u<0x143, 0xC>(v);
+  return v;
+}
+// Inclusive scans over the threads, of one value or of two; the totals go to all.
+template <class U, int W>
+struct Totals {
+  U of[W];
+  __device__ __forceinline__ void join(U& v, U& total, int wave) const {
+    U before = 0;
+    total = 0;
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_scan(v[n]);
-  __syncthreads();
-  if (lane == 63)
-#pragma unroll
-    for (int n = 0; n < N; ++n) sh[n][wave] = v[n];
-  __syncthreads();
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    u64 before = 0;
-    total[n] = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-      const u64 x = sh[n][w];
+    for (int w = 0; w < W; ++w) {
+      const U x = of[w];
       if (w < wave) before += x;
-      total[n] += x;
+      total += x;
     }
-    v[n] += before;
+    v += before;
   }
+};
+template <int NT, class U>
+__device__ __forceinline__ void block_scan(U& v, U& total) {
+  __shared__ Totals<U, NT / 64> sh;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  v = wave_scan(v);
+  __syncthreads();
+  if (lane == 63) sh.of[wave] = v;
+  __syncthreads();
+  sh.join(v, total, wave);
+}
+template <int NT, class U, class V>
+__device__ __forceinline__ void block_scan(U& u, U& total_u, V& v, V& total_v) {
+  __shared__ Totals<U, NT / 64> sh_u;
+  __shared__ Totals<V, NT / 64> sh_v;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  u = wave_scan(u);
+  v = wave_scan(v);
+  __syncthreads();
+  if (lane == 63) sh_u.of[wave] = u, sh_v.of[wave] = v;
+  __syncthreads();
+  sh_u.join(u, total_u, wave);
+  sh_v.join(v, total_v, wave);
 }
 
 // ---- histogram of the tokens [from, to) into LDS, REP copies by lane; returns
@@ -393,12 +420,14 @@ __device__ __forceinline__ uint32_t count_tokens(Tokens<T, NT>& tokens, const Ro
 template <int NT>
 struct Places {
   static constexpr int PB = kBins / NT;
-  u64 c_at[PB], c_to[PB], w_at[PB], w_to[PB];  // before and after each bin
-  u64 live, total;
-  u64 k;
-  u64 f_lo, f_hi;  // bounds of the count above the floor (equal: the count)
-  u64 gathered;  // tokens of the bins that are needed
-  int deepest;   // the last of them
+  uint32_t c_at[PB], c_to[PB];  // before and after each bin
+  u64 w_at[PB], w_to[PB];
+  uint32_t live;
+  u64 total;
+  uint32_t k;
+  uint32_t f_lo, f_hi;  // bounds of the count above the floor (equal: the count)
+  uint32_t gathered;    // tokens of the bins that are needed
+  int deepest;          // the last of them
 
   u64 w[PB];
   uint32_t c[PB];
@@ -409,33 +438,34 @@ struct Places {
   }
   // `need` [kBins] gets 1 for the bins to gather.
   __device__ void find(const Row& s, uint32_t over_floor, uint8_t* need) {
-    __shared__ u64 lohi[2], np[2];
+    __shared__ u64 lohi[2];
+    __shared__ uint32_t np[2];
     __shared__ int deep;
     if (threadIdx.x == 0) deep = 0;
     const int b0 = threadIdx.x * PB;
-    u64 sum[2] = {0, 0}, tot[2];
+    uint32_t sum_c = 0;
+    u64 sum_w = 0;
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
-      c_to[i] = sum[0] += c[i];
-      w_to[i] = sum[1] += w[i];
+      c_to[i] = sum_c += c[i];
+      w_to[i] = sum_w += w[i];
       need[b0 + i] = 0;
     }
-    const u64 own0 = sum[0], own1 = sum[1];
-    block_scan<NT, 2>(sum, tot);
+    const uint32_t own_c = sum_c;
+    const u64 own_w = sum_w;
+    block_scan<NT>(sum_c, live, sum_w, total);
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
-      c_to[i] += sum[0] - own0;
-      w_to[i] += sum[1] - own1;
+      c_to[i] += sum_c - own_c;
+      w_to[i] += sum_w - own_w;
       c_at[i] = c_to[i] - c[i];
       w_at[i] = w_to[i] - w[i];
     }
-    live = tot[0];
-    total = tot[1];
-    k = min((u64)s.k, live);
+    k = min((uint32_t)s.k, live);
     // Where a bin holds a place, the sum there is known to within the bin's
     // weight; the places that depend on it lie between the bins of the two
     // ends.  Nothing in the last bin weighs anything.
-    const auto bounds = [&](u64 count, double& lo, double& hi) {  // weight at `count`
+    const auto bounds = [&](uint32_t count, double& lo, double& hi) {  // weight at `count`
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < PB; ++i)
@@ -457,13 +487,13 @@ struct Places {
           if (c_at[i] < c_to[i]) need[b0 + i] = 1;
         }
       __syncthreads();
-      f_lo = max(lohi[0], 1ull);
-      f_hi = max(lohi[1], 1ull);
+      f_lo = max((uint32_t)lohi[0], 1u);
+      f_hi = max((uint32_t)lohi[1], 1u);
     } else {
-      f_lo = f_hi = s.floor_bin == kLast ? max((u64)over_floor, 1ull) : max(live, 1ull);
+      f_lo = f_hi = s.floor_bin == kLast ? max(over_floor, 1u) : max(live, 1u);
     }
     double lo = 0, hi = 0;
-    u64 n_lo = k, n_hi = k;  // bounds of the kept count
+    uint32_t n_lo = k, n_hi = k;  // bounds of the kept count
     if (s.top_p < 1.0) {
       bounds(k, lo, hi);
       lo *= s.top_p;
@@ -488,21 +518,19 @@ struct Places {
     const double d_lo = s.u * lo;
     if (n_hi != n_lo) bounds(n_hi, lo, hi);
     const double d_hi = s.u * hi;
-    u64 mine[1] = {0}, all[1];
+    before = 0;
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       if (c_at[i] < c_to[i] && (double)w_to[i] > d_lo && (double)w_at[i] <= d_hi) need[b0 + i] = 1;
       if (need[b0 + i]) {
-        mine[0] += c_to[i] - c_at[i];
+        before += c_to[i] - c_at[i];
         atomicMax(&deep, b0 + i);
       }
     }
-    block_scan<NT, 1>(mine, all);  // need[] and deep are complete behind it
+    block_scan<NT>(before, gathered);  // need[] and deep are complete behind it
     deepest = deep;
-    gathered = all[0];
-    before = mine[0];
   }
-  u64 before;  // gathered tokens up to and with this thread's bins
+  uint32_t before;  // gathered tokens up to and with this thread's bins
 };
 
 template <class T, int NT>
@@ -562,11 +590,11 @@ __device__ Found radix_find(const T* x, int V, const Row& s, bool by_weight, u64
     }
     __syncthreads();
     const u64 c = threadIdx.x < 256 ? hc[threadIdx.x] : 0, w = threadIdx.x < 256 ? hw[threadIdx.x] : 0;
-    u64 in[2] = {c, w}, tot[2];
-    block_scan<NT, 2>(in, tot);
-    const u64 to = by_weight ? f.weight + in[1] : f.count + in[0], at = to - (by_weight ? w : c);
+    u64 to_c = c, to_w = w, all_c, all_w;
+    block_scan<NT>(to_c, all_c, to_w, all_w);
+    const u64 to = by_weight ? f.weight + to_w : f.count + to_c, at = to - (by_weight ? w : c);
     if (c > 0 && to > target && at <= target)
-      got = Found{f.count + in[0] - c, f.weight + in[1] - w, f.key | (uint32_t)threadIdx.x << sft};
+      got = Found{f.count + to_c - c, f.weight + to_w - w, f.key | (uint32_t)threadIdx.x << sft};
     __syncthreads();
     f = got;
   }
@@ -723,10 +751,10 @@ __device__ void draw_by_digits(const SampleArgs& a, int r, const T* x, const Row
   for (int i0 = 0; i0 < V; i0 += NT) {
     const int i = i0 + tid;
     const bool eq = i < V && s.seen(logit(x, i)) == best;
-    u64 to[1] = {eq}, here[1];
-    block_scan<NT, 1>(to, here);
-    if (eq && seen + to[0] - 1 == want) at_s = i;
-    seen += here[0];
+    uint32_t to = eq, here;
+    block_scan<NT>(to, here);
+    if (eq && seen + to - 1 == want) at_s = i;
+    seen += here;
     if (seen > want) break;
   }
   __syncthreads();
@@ -773,20 +801,20 @@ __device__ void answer(const SampleArgs& a, int r, const T* x, const Row& s, con
   // Running sums over the gathered tokens, `per` in a row a thread; taken off
   // where a bin begins, they are sums within the bin.
   const int per = (G + NT - 1) / NT, i0 = min(tid * per, G), i1 = min(i0 + per, G);
-  u64 sum[1] = {0}, tot[1];
+  u64 sum = 0, tot;
   uint32_t over = 0;
   for (int i = i0; i < i1; ++i) {
     const double y = s.y(logit_of(m.cand[i]));
     const int b = Row::bin(y);
     const u64 w = b < kLast ? s.weight(y) : 0;
-    sum[0] += w;
+    sum += w;
     m.w[i] = w;
     over += b == s.floor_bin && y >= s.floor_y;
   }
   if (over) atomicAdd(&z.over, over);
-  const u64 own = sum[0];
-  block_scan<NT, 1>(sum, tot);
-  u64 at = sum[0] - own;
+  const u64 own = sum;
+  block_scan<NT>(sum, tot);
+  u64 at = sum - own;
   for (int i = i0; i < i1; ++i) {
     const int b = Row::bin(s.y(logit_of(m.cand[i])));
     if ((uint32_t)i == z.bin.first[b]) z.bin.start[b] = at;
@@ -815,24 +843,25 @@ __device__ __forceinline__ void answer_flat(const SampleArgs& a, int r, const Ro
   const int tid = threadIdx.x;
   sort_tokens<NT>(m, G);
   const int per = (G + NT - 1) / NT, i0 = min(tid * per, G), i1 = min(i0 + per, G);
-  u64 sum[2] = {0, 0}, tot[2];
+  u64 sum = 0, tot;
+  uint32_t over = 0, above;
   for (int i = i0; i < i1; ++i) {
     const double y = s.y(logit_of(m.cand[i]));
     const u64 w = Row::bin(y) < kLast ? s.weight(y) : 0;
-    sum[0] += w;
-    sum[1] += y >= s.floor_y;
+    sum += w;
+    over += y >= s.floor_y;
     m.w[i] = w;
   }
-  const u64 own = sum[0];
-  block_scan<NT, 2>(sum, tot);
-  u64 at = sum[0] - own;
+  const u64 own = sum;
+  block_scan<NT>(over, above, sum, tot);
+  u64 at = sum - own;
   for (int i = i0; i < i1; ++i) {
     at += m.w[i];
     m.run[i] = at;
     m.count[i] = i + 1;
   }
   __syncthreads();
-  draw_from<NT>(a, r, s, m, G, min((u64)s.k, (u64)G), max(tot[1], 1ull), res, [](u64) {});
+  draw_from<NT>(a, r, s, m, G, min((u64)s.k, (u64)G), max(above, 1u), res, [](u64) {});
 }
 
 // A bound that at least k of the values (PV a thread, -inf for none) reach,
@@ -1126,18 +1155,19 @@ __device__ __forceinline__ void answer_by_groups(const SampleArgs& a, int r, con
   }
   // very many equal logits: from the whole row, past the groups' bound
   s.least = s.inf ? kLeast : least;
-  u64 sum[2] = {0, 0}, tot[2], over[1] = {0}, all[1];
+  u64 sum = 0, total;
+  uint32_t live_n = 0, live, over = 0, above;
   Tokens<T, kThreads> tokens(x, 0, a.vocab);
   tokens.each([&](int, float v) {
     if (!(v >= s.least)) return;
     const double y = s.y(s.seen(v));
-    sum[0] += 1;
-    sum[1] += Row::bin(y) < kLast ? s.weight(y) : 0;
-    over[0] += y >= s.floor_y;
+    ++live_n;
+    sum += Row::bin(y) < kLast ? s.weight(y) : 0;
+    over += y >= s.floor_y;
   });
-  block_scan<kThreads, 2>(sum, tot);
-  block_scan<kThreads, 1>(over, all);
-  draw_by_digits<T, kThreads>(a, r, x, s, tot[0], tot[1], min((u64)s.k, tot[0]), max(all[0], 1ull), digits);
+  block_scan<kThreads>(live_n, live, sum, total);
+  block_scan<kThreads>(over, above);
+  draw_by_digits<T, kThreads>(a, r, x, s, live, total, min((uint32_t)s.k, live), max(above, 1u), digits);
 }
 
 template <class T>
