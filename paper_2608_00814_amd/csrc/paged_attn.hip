@@ -27,6 +27,14 @@ __device__ __forceinline__ Seq seq_of(const Paged& p, int b, int R) {
   return s;
 }
 
+// Whether query rows against so many keys go to wide blocks.
+__device__ __forceinline__ bool wide_rows(const PlanShape& s, int rows, int keys) {
+  return rows > s.narrow && (s.narrow == 0 || keys > kShortTiles * kTileKeys);
+}
+__device__ __forceinline__ int keys_of(const Paged& p, const Seq& q) {
+  return min(q.len + (p.W ? min(q.rows, 64 * p.W) : q.rows), p.own_cap);
+}
+
 // What a thread of the plan looks at: one shared block, or one sequence.
 struct Entry {
   Seq q;
@@ -53,7 +61,7 @@ __device__ __forceinline__ Entry entry_of(const Paged& p, const PlanShape& s, in
   x.shared = e < shared;
   x.q = x.shared ? Seq{0, 0, 0} : seq_of(p, e - shared, R);
   x.rows = x.shared ? min(sblock, stack - e * sblock) : x.q.rows * p.G;
-  x.wide = x.shared ? sblock > s.narrow : x.rows > s.narrow;
+  x.wide = x.shared ? sblock > s.narrow : wide_rows(s, x.rows, keys_of(p, x.q));
   x.block = x.wide ? s.wide : s.narrow;
   x.n = x.rows > 0 ? (x.rows + x.block - 1) / x.block : 0;
   return x;
@@ -155,7 +163,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
   const int tid = threadIdx.x;
   const int R = min(max(p.row_start[p.n_seqs], 0), p.n_rows);
   const int stack = R * p.G;  // query rows of a KV head
-  const bool swide = stack > s.narrow;
+  const bool swide = wide_rows(s, stack, p.shared_len);
   const int sblock = swide ? s.wide : s.narrow;
   const int sblocks = p.shared_len > 0 && stack > 0 ? (stack + sblock - 1) / sblock : 0;
   // entries: a narrow shared block, then the sequences
@@ -267,7 +275,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
       it.flags = (x.shared ? kShared : 0) | (direct ? kDirect : 0);
       it.seq = x.shared ? 0 : e - lead;
       it.row0 = x.q.row0;
-      it.q0 = j * x.block;
+      it.q0 = (x.shared ? e : j) * x.block;  // an entry is one shared block
       it.nq = nq;
       it.limit = limit;
       it.len = x.shared ? limit : x.q.len;
@@ -331,7 +339,7 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, ui
   const int rows = q.rows * p.G, at = x - q.row0 * p.G;
   RowSlots o{};
   if (at >= 0 && at < rows) {
-    const int block = rows > s.narrow ? s.wide : s.narrow;
+    const int block = wide_rows(s, rows, keys_of(p, q)) ? s.wide : s.narrow;
     const long long blk = reinterpret_cast<const int*>(plan + s.off_seqs)[lo] + at / block;
     if (blk < s.max_blocks) {
       const BlockSlots d = reinterpret_cast<const BlockSlots*>(plan + s.off_blocks)[blk];
@@ -541,28 +549,30 @@ __global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
 }
 
 // ------------------------------------------------------------------- join
-// Adds the parts of every row: 4 waves, one for each of 4 accumulator pieces of
-// a group of stacked query rows and KV head; a lane joins 4 columns of one row
-// over the row's shared and own slots.  Lane (c, q) of a piece holds row c and,
-// in float32 (groups of 16), columns 64 (piece / 4) + 16 q + 4 e + piece % 4;
-// in bf16 (groups of 32) columns 8 piece + 4 q + e.  Bound by latency: the
-// plan's head and the row's slots are asked for together, then four slots at a
-// time: 5 us for 64 rows of 32 heads, 7 for 385.
-template <class T, int D>
+// Adds the parts of every row.  A wave has one accumulator piece of a group of
+// stacked query rows and KV head, and a lane 4 columns of one row over the
+// row's shared and own slots.  Lane (c, q) of a piece holds row c and, in
+// float32 (groups of 16), columns 64 (piece / 4) + 16 q + 4 e + piece % 4; in
+// bf16 (groups of 32) columns 8 piece + 4 q + e.  Bound by latency: the plan's
+// head and the row's slots are asked for together, then four slots at a time:
+// 5 us for 64 rows of 32 heads, 7 for 385.  Few rows may be split over hundreds
+// of slots; then four waves share a piece's (PAR), eight slots at a time each.
+template <class T, int D, int PAR>
 __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int GR = BF ? 32 : 16, NP = D * GR / 256;
-  constexpr int AT_ONCE = 4;
+  constexpr int AT_ONCE = PAR == 1 ? 4 : 8, PIECES = 4 / PAR;  // of a workgroup
   const Paged& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane % GR, qd = lane / GR;
-  const int w = blockIdx.x / (NP / 4), pc = 4 * (blockIdx.x % (NP / 4)) + wave;
+  const int w = blockIdx.x / (NP / PIECES), pc = PIECES * (blockIdx.x % (NP / PIECES)) + wave % PIECES;
+  const int share = wave / PIECES;
   const int g = w % p.Hkv, x = (w / p.Hkv) * GR + c;
   const int i = x / p.G, h = g * p.G + x - i * p.G;
   const PlanHead head = load_head(a);
   const RowSlots rs = reinterpret_cast<const RowSlots*>(a.plan + a.off_rows)[min(x, p.n_rows * p.G - 1)];
   const bool fits = plan_fits(head, a.want);
-  if (i >= (fits ? head.rows : min(p.row_start[p.n_seqs], p.n_rows))) return;
+  const bool in = i < (fits ? head.rows : min(p.row_start[p.n_seqs], p.n_rows));
   T* const orow = (T*)a.out + ((size_t)i * p.Hq + h) * D;
   const auto put = [&](f32x4 o) {
     if constexpr (BF)
@@ -573,41 +583,60 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
   };
   if (!fits) {
     const float nan = __builtin_nanf("");
-    put(f32x4{nan, nan, nan, nan});
+    if (in && share == 0) put(f32x4{nan, nan, nan, nan});
     return;
   }
-  const int n0 = rs.part[0].splits, n = n0 + rs.part[1].splits;
-  if (rs.part[1].splits == 0) return;  // written by its item
+  const int n0 = rs.part[0].splits;
+  const int n = in && rs.part[1].splits > 0 ? n0 + rs.part[1].splits : 0;  // 0: written by its item
   float m = -INFINITY, den = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < n; s += AT_ONCE) {
-    f32x2_t ml[AT_ONCE];
-    f32x4 o[AT_ONCE];
-#pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {  // past the last one: that again
-      const int t = min(s + k, n - 1);
-      const RowSlots::Part& r = rs.part[t < n0 ? 0 : 1];
-      const long long slot = r.slot + (long long)(t < n0 ? t : t - n0) * r.stride;
-      const size_t sl = (size_t)min(slot, a.max_slots - 1) * p.Hkv + g;
-      ml[k] = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * GR + r.row];
-      o[k] = reinterpret_cast<const f32x4*>(a.part_o)[(sl * NP + pc) * 64 + GR * qd + r.row];
-    }
+  // adds N parts with their maxima and sums
+  const auto add = [&](auto& ms, auto& dens, auto& os) {
+    constexpr int N = sizeof(ms) / sizeof(float);
     float mn = m;
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) mn = fmaxf(mn, ml[k][0]);
+    for (int k = 0; k < N; ++k) mn = fmaxf(mn, ms[k]);
     const float base = mn == -INFINITY ? 0.f : mn;
     const float wa = exp2f(m - base);
     den *= wa;
     acc *= wa;
 #pragma unroll
-    for (int k = 0; k < AT_ONCE; ++k) {
-      const float wb = s + k < n ? exp2f(ml[k][0] - base) : 0.f;
-      if (s + k < n) den += ml[k][1] * wb;
-      if (wb > 0.f) acc += o[k] * wb;  // zero times an infinite sum is not zero
+    for (int k = 0; k < N; ++k) {
+      const float wb = exp2f(ms[k] - base);
+      den += dens[k] * wb;
+      if (wb > 0.f) acc += os[k] * wb;  // zero times an infinite sum is not zero
     }
     m = mn;
+  };
+  for (int s = share * AT_ONCE; s < n; s += PAR * AT_ONCE) {
+    float ms[AT_ONCE], dens[AT_ONCE];
+    f32x4 o[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {  // past the last one: that again, without weight
+      const int t = min(s + k, n - 1);
+      const RowSlots::Part& r = rs.part[t < n0 ? 0 : 1];
+      const long long slot = r.slot + (long long)(t < n0 ? t : t - n0) * r.stride;
+      const size_t sl = (size_t)min(slot, a.max_slots - 1) * p.Hkv + g;
+      const f32x2_t ml = reinterpret_cast<const f32x2_t*>(a.part_ml)[sl * GR + r.row];
+      o[k] = reinterpret_cast<const f32x4*>(a.part_o)[(sl * NP + pc) * 64 + GR * qd + r.row];
+      ms[k] = s + k < n ? ml[0] : -INFINITY;
+      dens[k] = s + k < n ? ml[1] : 0.f;
+    }
+    add(ms, dens, o);
   }
-  put(acc * (den == 0.f ? 0.f : 1.f / den));
+  if constexpr (PAR > 1) {
+    __shared__ float ms_s[PAR][64], den_s[PAR][64];
+    __shared__ f32x4 o_s[PAR][64];
+    ms_s[share][lane] = m, den_s[share][lane] = den, o_s[share][lane] = acc;
+    __syncthreads();
+    if (share > 0) return;
+    float ms[PAR - 1], dens[PAR - 1];
+    f32x4 o[PAR - 1];
+#pragma unroll
+    for (int k = 0; k < PAR - 1; ++k) ms[k] = ms_s[k + 1][lane], dens[k] = den_s[k + 1][lane], o[k] = o_s[k + 1][lane];
+    add(ms, dens, o);
+  }
+  if (n > 0) put(acc * (den == 0.f ? 0.f : 1.f / den));
 }
 
 template <class T, int D>
@@ -616,7 +645,9 @@ void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
   if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
   else paged_attn_f32_kernel<D><<<items, 512, 0, st>>>(a);
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
-  join_kernel<T, D><<<(unsigned)(groups * a.p.Hkv * (D * s.group / 1024)), 256, 0, st>>>(a);
+  const long long blocks = groups * a.p.Hkv * (D * s.group / 1024);
+  if (blocks <= 2 * device_cus()) join_kernel<T, D, 4><<<(unsigned)(4 * blocks), 256, 0, st>>>(a);
+  else join_kernel<T, D, 1><<<(unsigned)blocks, 256, 0, st>>>(a);
 }
 
 size_t workspace_bytes(const ooo_paged_batch& b, const PlanShape& s) {

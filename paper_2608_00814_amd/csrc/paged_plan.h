@@ -4,9 +4,9 @@
 // The query rows of a KV head are stacked: row i of a sequence gives G query
 // rows i G .. i G + G - 1, one for each query head of the group.  A *block* is
 // a set of query rows that read the same keys:
-//   own blocks     up to `wide` consecutive query rows of one sequence (one
-//                  block of up to `narrow` where there are few), against the
-//                  sequence's own tokens;
+//   own blocks     up to `wide` consecutive query rows of one sequence, or up
+//                  to `narrow` where its rows are no more or its keys few,
+//                  against the sequence's own tokens;
 //   shared blocks  the same of the whole stack, against the shared prompt,
 //                  which is so read once for many sequences.
 // A KV head's work goes to `workers` workgroups, all on the chip at once:
@@ -35,6 +35,10 @@
 namespace ooo {
 
 constexpr int kTileKeys = 64;
+// Up to so many tiles of keys, 128 query rows are cheaper as four narrow blocks,
+// one wave's work each and eight at a time on a worker, than as a wide one,
+// whose start and end take longer than its tiles.
+constexpr int kShortTiles = 4;
 constexpr int kSplitMost = 4;  // extra items of the shared blocks: at most so many times the workers
 
 struct PlanShape {
@@ -96,9 +100,10 @@ inline PlanShape plan_shape(const ooo_paged_batch& b) {
   const long long G = b.n_q_heads / b.n_kv_heads, q = b.n_rows * G;
   const long long shared = b.shared_len > 0 ? (q + s.wide - 1) / s.wide : 0;
   const long long own = b.n_seqs + q / s.wide;  // a sequence's last block may be short
-  s.max_blocks = shared + own;
-  s.max_items_w = s.max_blocks + (kSplitMost + 1ll) * s.workers;
-  s.max_items_n = bf ? b.n_seqs + 1 + (long long)s.waves * s.workers : 0;
+  const long long narrow = bf ? b.n_seqs + q / s.narrow + (b.shared_len > 0 ? q / s.narrow + 1 : 0) : 0;
+  s.max_blocks = shared + own + narrow;
+  s.max_items_w = shared + own + (kSplitMost + 1ll) * s.workers;
+  s.max_items_n = bf ? narrow + (long long)s.waves * s.workers : 0;
   const long long per_wide = s.wide / s.group, runs = s.workers * (per_wide + s.waves);
   s.max_slots = b.n_seqs + 1 + q / s.group + (shared + (long long)kSplitMost * s.workers) * per_wide + runs;
   const auto up = [](long long n) { return (n + 63) / 64 * 64; };
