@@ -19,8 +19,10 @@
 // computed in double: with float32's rounding, of 152064 nearly equal tokens
 // one draw in 50 would go to a neighbour.
 //
-// Rows of up to kOneBlock tokens are one workgroup's work.  Longer ones are
-// cut into chunks over many workgroups.  The first launch finds the largest
+// Rows of up to kOneBlock tokens are one workgroup's work: one launch, where
+// chunks take four (240 rows of 11053: 24 us, 46 in chunks; 17 rows of 17940:
+// 27 and 34; 28 rows of 30630: 39 and 36).  Longer ones are cut into chunks
+// over many workgroups.  The first launch finds the largest
 // logit and those of up to kGroups disjoint groups of tokens.
 //  * With top-k (or greedily), no token below the k-th largest of the groups'
 //    largest logits can be kept, and only the groups that reach that are read
@@ -53,7 +55,7 @@ constexpr int kLast = kBins - 1;     // the bin of what lies past the range and 
 constexpr double kRange = 46.0;      // log2 of the least weight of the other bins
 constexpr int kGather = 2048;        // tokens of the bins that are looked at closely
 constexpr int kReplicas = 2;         // of a chunk's histogram, by lane: fewer lanes meet in one bin
-constexpr int kOneBlock = 8192;      // tokens
+constexpr int kOneBlock = 32768;      // tokens
 constexpr int kGroups = 4096;        // groups of a long row, at most
 constexpr int kFlat = 1024;          // tokens that are answered from without bins
 constexpr int kFlatK = 512;          // the largest top-k that goes by its groups
