@@ -367,8 +367,8 @@ __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cas
 // dt % 4.  Bound by latency where it is used (float32 is the small option): 53
 // rows of three tries over 128 + 100 tokens take 6.7 us.
 template <int D>
-__global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
-  constexpr int NW = 8;
+__global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_kernel(PagedAttnArgs a) {
+  constexpr int NW = kF32Waves;
   constexpr int KS = D / 16;
   __shared__ f32x4 o_s[NW][KS][64];
   __shared__ f32x2_t ml_s[NW][16];
@@ -525,25 +525,31 @@ __global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
       if (qd == 0) ml_s[wave][c] = f32x2_t{m, l_run};
       __syncthreads();
     }
-    if (wave >= KS || !on) return;  // wave dt adds accumulator dt
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+    if (!on) return;
+    float wgt[NW];
+#pragma unroll
     for (int w = 0; w < NW; ++w) {
       const f32x2_t ml = ml_s[w][c];
-      const float wgt = exp2f(ml[0] - base);
-      den += wgt * ml[1];
-      acc += wgt * o_s[w][wave][lane];
+      wgt[w] = exp2f(ml[0] - base);
+      den += wgt[w] * ml[1];
     }
     if (poison) den = __builtin_nanf("");
-    if (it.flags & kDirect) {
-      const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees no key is zero
-      float* orow = (float*)a.out + (row * p.Hq + head_q) * D + 64 * (wave >> 2) + 16 * qd + (wave & 3);
+    const float inv = den == 0.f ? 0.f : 1.f / den;  // a row that sees no key is zero
 #pragma unroll
-      for (int r = 0; r < 4; ++r) orow[4 * r] = acc[r] * inv;
-    } else if (it.slot < a.max_slots) {
-      const size_t sl = (size_t)it.slot * p.Hkv + g;
-      reinterpret_cast<f32x4*>(a.part_o)[(sl * KS + wave) * 64 + lane] = acc;
-      if (wave == 0 && qd == 0) reinterpret_cast<f32x2_t*>(a.part_ml)[sl * 16 + c] = f32x2_t{m, den};
+    for (int dt0 = 0; dt0 < KS; dt0 += NW) {  // a wave adds every fourth accumulator
+      const int dt = dt0 + wave;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) acc += wgt[w] * o_s[w][dt][lane];
+      if (it.flags & kDirect) {
+        float* orow = (float*)a.out + (row * p.Hq + head_q) * D + 64 * (dt >> 2) + 16 * qd + (dt & 3);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) orow[4 * r] = acc[r] * inv;
+      } else if (it.slot < a.max_slots) {
+        const size_t sl = (size_t)it.slot * p.Hkv + g;
+        reinterpret_cast<f32x4*>(a.part_o)[(sl * KS + dt) * 64 + lane] = acc;
+        if (dt == 0 && qd == 0) reinterpret_cast<f32x2_t*>(a.part_ml)[sl * 16 + c] = f32x2_t{m, den};
+      }
     }
   });
 }
@@ -556,7 +562,10 @@ __global__ __launch_bounds__(512) void paged_attn_f32_kernel(PagedAttnArgs a) {
 // bf16 (groups of 32) columns 8 piece + 4 q + e.  Bound by latency: the plan's
 // head and the row's slots are asked for together, then four slots at a time:
 // 5 us for 64 rows of 32 heads, 7 for 385.  Few rows may be split over hundreds
-// of slots; then four waves share a piece's (PAR), eight slots at a time each.
+// of slots; then four waves share a piece's (PAR), eight slots at a time each:
+// the call for two rows over a 22k prompt takes 51 us, 130 with one.  More rows
+// have few parts, and four times the waves cost more: 60 us, not 47, for 1145
+// rows of four prompts.  Hence the bound on the workgroups in launch_attn.
 template <class T, int D, int PAR>
 __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
   constexpr bool BF = sizeof(T) == 2;
@@ -643,7 +652,7 @@ template <class T, int D>
 void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
   const unsigned items = (unsigned)(s.workers * a.p.Hkv);
   if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
-  else paged_attn_f32_kernel<D><<<items, 512, 0, st>>>(a);
+  else paged_attn_f32_kernel<D><<<items, 64 * kF32Waves, 0, st>>>(a);
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
   const long long blocks = groups * a.p.Hkv * (D * s.group / 1024);
   if (blocks <= 2 * device_cus()) join_kernel<T, D, 4><<<(unsigned)(4 * blocks), 256, 0, st>>>(a);

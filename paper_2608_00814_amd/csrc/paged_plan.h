@@ -37,9 +37,17 @@ namespace ooo {
 constexpr int kTileKeys = 64;
 // Up to so many tiles of keys, 128 query rows are cheaper as four narrow blocks,
 // one wave's work each and eight at a time on a worker, than as a wide one,
-// whose start and end take longer than its tiles.
+// whose start and end take longer than its tiles (38 tries of 46 rows with no
+// prompt to speak of: 60 us in wide blocks, 46 so; 8 tiles are no better).
 constexpr int kShortTiles = 4;
 constexpr int kSplitMost = 4;  // extra items of the shared blocks: at most so many times the workers
+
+// Waves of a float32 worker, and workers on a CU at once (the kernel keeps 168
+// registers at head_dim 64 and 248 at 128; forced to 168, it spills and takes
+// twice the time, and eight waves a worker, one of which fills a CU, take 10%
+// longer).
+constexpr int kF32Waves = 4;
+__host__ __device__ constexpr int f32_per_cu(int head_dim) { return head_dim == 64 ? 3 : 2; }
 
 struct PlanShape {
   int narrow, wide, group;  // query rows (narrow 0: there are no narrow blocks)
@@ -95,7 +103,7 @@ inline PlanShape plan_shape(const ooo_paged_batch& b) {
   s.narrow = bf ? 32 : 0;
   s.wide = bf ? 128 : 16;
   s.waves = bf ? 8 : 0;
-  s.workers = (bf ? 1 : 2) * device_cus() / b.n_kv_heads;
+  s.workers = (bf ? 1 : f32_per_cu(b.head_dim)) * device_cus() / b.n_kv_heads;
   if (s.workers < 1) s.workers = 1;
   const long long G = b.n_q_heads / b.n_kv_heads, q = b.n_rows * G;
   const long long shared = b.shared_len > 0 ? (q + s.wide - 1) / s.wide : 0;
