@@ -149,7 +149,7 @@ __device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int
   return best;
 }
 
-// One workgroup, 15 us for up to 256 sequences, once a step.  First the
+// One workgroup, 15 to 30 us for up to 256 sequences, once a step.  First the
 // lengths, from them the deal, then the items and slots of every entry behind
 // those of the entries before it.
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, int half_dim,
@@ -365,7 +365,7 @@ __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cas
 // order (lane (c, q) holds row c's scores of keys 4q .. 4q + 3).  Lane (c, q)
 // of the O^T accumulator dt holds row c, columns 64 (dt / 4) + 16 q + 4 r +
 // dt % 4.  Bound by latency where it is used (float32 is the small option): 53
-// rows of three tries over 128 + 100 tokens take 6.7 us.
+// rows of three tries over 128 + 100 tokens take 6.3 us.
 template <int D>
 __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int NW = kF32Waves;
