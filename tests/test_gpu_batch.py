@@ -296,6 +296,58 @@ def test_attn_more_heads_than_work_is_shared_over(dt, heads):
         b.check(b.attend())
 
 
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("shared,page", [(0, 16), (333, 32), (1000, 128)])
+def test_attn_tries_over_long_sequences(dt, D, shared, page):
+    """Many rows with masks behind more keys than a short block has; masks that
+    begin inside a tile, blocks whose last rows are few."""
+    r = random.Random(D)
+    rows, lens = [64, 3, 150, 40, 33], [300, 700, 261, 1000, 321]
+    mask = bh.trie_masks(r, rows, 3)[0]
+    b = Batch(dt, 8, 2, D, page, rows, lens, shared=shared, mask=mask, pad=1, seed=shared)
+    b.check(b.attend())
+    c = Batch(dt, 8, 2, D, page, rows, lens, shared=shared, seed=shared + 1)
+    c.check(c.attend())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attn_what_is_not_seen_behind_long_sequences(dt, D):
+    r = random.Random(2)
+    rows, lens, shared = [90, 34], [300, 417], 410
+    mask = bh.trie_masks(r, rows, 2)[0]
+    b = Batch(dt, 8, 2, D, 16, rows, lens, shared=shared, mask=mask, seed=4)
+    for ids, n in ((b.table[0], 390), (b.table[1], 451), (b.shared_ids, shared)):
+        for t in range(n, (n + 15) // 16 * 16):
+            pg, sl = ob.place(ids, t, 16)
+            b.k[pg, :, sl], b.v[pg, :, sl] = float("nan"), float("inf")
+    b.check(b.attend())
+    for j, bad in ((7, float("inf")), (66, float("nan")), (89, float("-inf"))):
+        pg, sl = ob.place(b.table[0], 300 + j, 16)
+        b.v[pg, :, sl] = bad
+        if j == 66:
+            b.k[pg, :, sl] = bad
+    got = f64(b.attend())
+    ref, A, S = b.reference()
+    hit = np.zeros(b.total, bool)
+    hit[:90] = np.array([[(int(mask[x, j // 64]) >> (j % 64)) & 1 for j in (7, 66, 89)] for x in range(90)]).any(axis=1)
+    assert hit[:90].any() and not hit[:90].all()
+    assert not np.isfinite(got[hit]).any(), "a seen value that is not finite was lost"
+    with np.errstate(invalid="ignore"):
+        err, lim = np.abs(got[~hit] - ref[~hit]), b.bound(ref, A, S)[~hit]
+    assert (err <= lim).all()
+
+
+def test_attn_bad_pages_of_long_sequences_are_visible():
+    b = Batch("bf16", 4, 2, 128, 16, [40, 1, 50], [600, 40, 900], shared=700)
+    good = f64(b.attend())
+    b.d_table[2, 30] = -1
+    got = f64(b.attend())
+    assert np.isnan(got[41:]).all() and np.array_equal(got[:41], good[:41])
+    b.d_shared[20] = b.k.shape[0]
+    assert np.isnan(f64(b.attend())).all()
+
+
 def test_attn_two_batches_on_two_streams():
     """Captured together and replayed, each with its own plan and workspace."""
     bs = [Batch("bf16", 8, 2, 128, 16, rows, lens, shared=sh, seed=sh)
