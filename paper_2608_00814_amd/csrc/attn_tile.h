@@ -64,6 +64,12 @@ __device__ __forceinline__ float max3f(float a, float b, float c) {
   return r;
 }
 
+// s plus the two bf16 values packed in x: their dot product with ones.
+__device__ __forceinline__ float add_bf16x2(uint32_t x, float s) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, x), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), s,
+                                         false);
+}
+
 // The end of the wait for a matrix product's result: the compiler knows how
 // long a vector instruction of its own has to stay behind the product that it
 // reads, but not one in inline asm (max3f), which would read what was there

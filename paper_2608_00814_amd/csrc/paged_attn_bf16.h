@@ -223,7 +223,9 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
   };
   // Probabilities, two at a time, each pair behind the next pair's exponents;
   // between(k) goes with pair k.  They go into the product rounded to bf16, the
-  // matrix cores' operand.
+  // matrix cores' operand, and the rounded ones into the sum: the weights that
+  // multiply V then sum to one, and the rounding (half a step, 2^-8, each)
+  // moves an output by that share of sum p |v - out| alone.
   auto weights = [&](const f32x16& s, float m_use, bf16x8 (&pf)[2], auto between) OOO_INLINE {
     float x[2] = {fmaf(s[0], scale, -m_use), fmaf(s[1], scale, -m_use)};
     float pr[2][2], ps[2] = {0.f, 0.f};
@@ -242,9 +244,8 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
       }
       if (k > 0) {
         const float* e = pr[(k - 1) & 1];
-        ps[0] += e[0];
-        ps[1] += e[1];
         pk[(k - 1) / 4][(k - 1) % 4] = pack_bf16x2(e[0], e[1]);
+        ps[k & 1] = add_bf16x2(pk[(k - 1) / 4][(k - 1) % 4], ps[k & 1]);
       }
     }
     pf[0] = as_bf16x8(pk[0]);

@@ -375,6 +375,32 @@ def test_attn_two_batches_on_two_streams():
             assert torch.equal(out, w)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rows,lens,shared", [([1, 2], [500, 64], 0), ([1] * 5, [200, 31, 0, 96, 33], 320),
+                                              ([60, 40], [300, 416], 0), ([64], [512], 640)])
+def test_attn_weights_sum_to_one(D, rows, lens, shared):
+    """Where all keys have the same v it comes out unchanged, however the
+    probabilities were rounded: numerator and denominator hold the same ones.
+    Every 32nd key scores 0, the others' probabilities lie 0.0035 of themselves
+    above a bf16 value, all to one side; v lies just below 2, where half a step
+    is 0.00196 of it.  What is left are float32 roundings, under 3 (n + 64) of
+    them of 2^-24 each (sums of n terms in O and in l, factors between parts):
+    0.0002 at n = 1152."""
+    b = Batch("bf16", 8, 2, D, 16, rows, lens, shared=shared)
+    b.scale = -math.log(0.50175)  # a key of -1 gets exp(-scale) = 0.50175 of a key of 0
+    b.q.zero_()
+    b.q[..., 0] = 1
+    b.k.zero_()
+    for ids, n in [(b.shared_ids, shared)] + [(t, n + m) for t, n, m in zip(b.table, b.rows, b.lens)]:
+        for t in range(n):
+            pg, sl = ob.place(ids, t, 16)
+            b.k[pg, :, sl, 0] = 0 if t % 32 == 0 else -1
+    c = torch.tensor([1.9921875, -1.984375, 0.99609375, -3.984375], device="cuda").repeat(D // 4).to(b.dt)
+    b.v.copy_(c.expand_as(b.v))
+    out = b.attend()
+    assert torch.equal(out[:b.total], c.expand(b.total, 8, D))
+
+
 # ----------------------------------------------------------------- compact
 
 
