@@ -190,9 +190,10 @@ struct Row {
   __device__ __forceinline__ float seen(float x) const {
     return !inf || x == -INFINITY ? x : x == INFINITY ? 0.f : -0x1p127f;
   }
-  // log2 of the weight, at least -64
-  __device__ __forceinline__ double y(float x) const { return fmax(((double)x - (double)M) * c, -64.0); }
-  static __device__ __forceinline__ int bin(double y) { return min((int)(y * -(kLast / kRange)), kLast); }
+  // log2 of the weight.  It may lie far below all bins (a floor does so too:
+  // min_p goes down to 2^-149), and weighs nothing from -64 on.
+  __device__ __forceinline__ double y(float x) const { return ((double)x - (double)M) * c; }
+  static __device__ __forceinline__ int bin(double y) { return min((int)(fmax(y, -64.0) * -(kLast / kRange)), kLast); }
   // 2^y 2^shift rounded to a whole number.  2^f, |f| <= 1/2: the polynomial of
   // degree 8 through its values at the Chebyshev nodes (off by 1.1e-12 at
   // most, exact at 0); adding 2^52 rounds to nearest and leaves the number in
@@ -245,7 +246,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, const Settings& set) 
   s.k = greedy ? 1 : set.k > 0 ? set.k : a.vocab;
   s.top_p = set.top_p < 1.f ? fmax((double)set.top_p, 0.0) : set.top_p >= 1.f ? 1.0 : 0.0;
   s.floor_y = set.min_p > 0.f ? log2((double)set.min_p) : -INFINITY;
-  s.floor_bin = s.floor_y == -INFINITY ? kBins : Row::bin(fmax(fmin(s.floor_y, 0.0), -64.0));
+  s.floor_bin = s.floor_y == -INFINITY ? kBins : Row::bin(fmin(s.floor_y, 0.0));
   s.u = set.u > 0.f ? fmin((double)set.u, 1.0 - 0x1p-24) : 0.0;
   s.shift = a.shift;
   return s;

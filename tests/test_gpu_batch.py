@@ -515,6 +515,24 @@ def test_sample_extreme_settings():
                m=[0, 0, 1e-6, 0, 1e-30, -1, 0, 1e-9], u=[1 - 2.0 ** -24] * 8)
 
 
+@pytest.mark.parametrize("V", [5, 400, 3000, 40000])
+def test_sample_counts_above_the_least_floors(V):
+    """min_p down to the least float32 over logits far below the largest one:
+    tokens of such weights are counted by their logits."""
+    r = np.random.default_rng(V)
+    x = np.full((7, V), -np.inf, np.float32)
+    x[:, :5] = [0, -1, -60, -75, -200]
+    x[1:4] = r.uniform(-300, 0, (3, V))
+    x[3, V // 2] = np.inf
+    x[4] = np.where(np.arange(V) < V - 2, 0.0, -150.0)  # nearly all equal
+    x[5] = np.where(np.arange(V) % 3 == 0, np.inf, r.uniform(-300, 0, V))
+    x[6] = np.where(np.arange(V) % 2 == 0, -30.0, r.uniform(-100, -30, V))
+    for T, m in ((1.0, 1e-30), (0.1, 1e-30), (1.0, 1e-45), (3.0, 1e-18), (1.0, 1e-12))[:5 if V < 40000 else 3]:
+        for k in (0, 3, 100, 600):
+            run_sample(x, T=[T] * 7, k=[k] * 7, m=[m] * 7, u=[0.0, 0.9, 0.5, 0.3, 0.999, 0.7, 0.1])
+        run_sample(x, T=[T] * 7, p=[0.9] * 7, m=[m] * 7, u=[0.0, 0.9, 0.5, 0.3, 0.999, 0.7, 0.1])
+
+
 # ---------------------------------------------------------------- together
 
 
