@@ -142,7 +142,8 @@ int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, 
  *   plan      of ooo_paged_plan for this batch.  A plan that was made for
  *             other sizes gives NaN rows; lengths come from the plan
  *   q         [n_rows][n_q_heads][head_dim] (16-byte aligned, as the pools and out)
- *   scale     score scale, normally 1/sqrt(head_dim)
+ *   scale     score scale, normally 1/sqrt(head_dim); any finite one (times
+ *             log2(e) too): 0 weighs all seen keys alike
  *   out       [n_rows][n_q_heads][head_dim], the type of q; must not alias
  *   workspace, ws_bytes   ooo_paged_attn_workspace(batch) bytes (16-byte
  *             aligned; on the same sizes as ooo_paged_plan_bytes)

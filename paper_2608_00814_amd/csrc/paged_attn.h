@@ -19,7 +19,7 @@ struct PagedAttnArgs {
   float* part_o;        // [slot][Hkv] groups in fragment order
   float* part_ml;       // [slot][Hkv][group] (m, l)
   long long max_slots;
-  float scale_log2e;
+  float scale_log2e;    // bf16: its size
 };
 
 // Memory that no kernel writes while it is read here, the same address in the

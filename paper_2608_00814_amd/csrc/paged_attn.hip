@@ -649,10 +649,14 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
 }
 
 template <class T, int D>
-void launch_attn(const PagedAttnArgs& a, const PlanShape& s, hipStream_t st) {
+void launch_attn(const PagedAttnArgs& a, const PlanShape& s, bool neg, hipStream_t st) {
   const unsigned items = (unsigned)(s.workers * a.p.Hkv);
-  if constexpr (sizeof(T) == 2) paged_attn_bf16_kernel<D><<<items, 64 * kPagedWaves, 0, st>>>(a);
-  else paged_attn_f32_kernel<D><<<items, 64 * kF32Waves, 0, st>>>(a);
+  if constexpr (sizeof(T) == 2) {
+    if (neg) paged_attn_bf16_kernel<D, true><<<items, 64 * kPagedWaves, 0, st>>>(a);
+    else paged_attn_bf16_kernel<D, false><<<items, 64 * kPagedWaves, 0, st>>>(a);
+  } else {
+    paged_attn_f32_kernel<D><<<items, 64 * kF32Waves, 0, st>>>(a);
+  }
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
   const long long blocks = groups * a.p.Hkv * (D * s.group / 1024);
   if (blocks <= 2 * device_cus()) join_kernel<T, D, 4><<<(unsigned)(4 * blocks), 256, 0, st>>>(a);
@@ -711,6 +715,9 @@ extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, si
   OOO_REQUIRE(aligned16(plan) && aligned16(q) && aligned16(k_pages) && aligned16(v_pages) && aligned16(out) &&
                   aligned16(workspace),
               OOO_ERR_UNSUPPORTED, "ooo_paged_attn: a pointer is not 16-byte aligned");
+  const float scale_log2e = scale * 1.4426950408889634f;
+  OOO_REQUIRE(fabsf(scale_log2e) < INFINITY, OOO_ERR_INVALID, "ooo_paged_attn: scale %g is not finite in base 2",
+              (double)scale);
   const PlanShape s = plan_shape(*batch);
   OOO_REQUIRE(plan_grid_ok(*batch, s), OOO_ERR_UNSUPPORTED, "ooo_paged_attn: more than 2^30 workgroups");
   OOO_REQUIRE(plan_bytes >= (size_t)s.bytes, OOO_ERR_CAPACITY, "ooo_paged_attn: plan of %lld bytes needed (got %zu)",
@@ -735,13 +742,20 @@ extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, si
   a.part_o = (float*)workspace;
   a.part_ml = a.part_o + (size_t)s.max_slots * batch->n_kv_heads * s.group * batch->head_dim;
   a.max_slots = s.max_slots;
-  a.scale_log2e = scale * 1.4426950408889634f;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const bool bf = batch->dt == OOO_BF16, wide = batch->head_dim == 128;
-  if (bf && wide) launch_attn<uint16_t, 128>(a, s, st);
-  else if (bf) launch_attn<uint16_t, 64>(a, s, st);
-  else if (wide) launch_attn<float, 128>(a, s, st);
-  else launch_attn<float, 64>(a, s, st);
+  a.scale_log2e = scale_log2e;
+  if (bf) {
+    // The bf16 kernel scales scores that are -inf where a key is not seen: by a
+    // positive number.  In place of 0 the least one, 2^-149, which moves weights
+    // by less than 2^-21 of themselves.
+    a.scale_log2e = fmaxf(fabsf(scale_log2e), 0x1p-149f);
+  }
+  const bool neg = scale_log2e < 0.f;
+  if (bf && wide) launch_attn<uint16_t, 128>(a, s, neg, st);
+  else if (bf) launch_attn<uint16_t, 64>(a, s, neg, st);
+  else if (wide) launch_attn<float, 128>(a, s, neg, st);
+  else launch_attn<float, 64>(a, s, neg, st);
   const hipError_t e = hipGetLastError();
   OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "ooo_paged_attn: launch failed: %s", hipGetErrorString(e));
   return ooo::ok();

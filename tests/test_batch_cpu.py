@@ -113,6 +113,15 @@ def test_attn_and_plan_refusals():
     assert f(q=P + 2) == f(w=P + 4) == ooo.ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_attn_refuses_scales_that_are_not_finite(scale):
+    """3e38 log2(e) is past the largest float32."""
+    for dt in (ooo.BF16, ooo.F32):
+        a, L = ctypes.addressof(struct(dt=dt)), ooo.lib()
+        assert L.ooo_paged_attn(a, P, 1 << 40, P, P, P, scale, P, P, 1 << 40, None) == ooo.ERR_INVALID
+        assert "scale" in ooo.last_error()
+
+
 def test_size_queries_follow_sizes_alone():
     """More rows, sequences or shared tokens never need less."""
     L = ooo.lib()

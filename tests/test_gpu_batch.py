@@ -401,6 +401,20 @@ def test_attn_weights_sum_to_one(D, rows, lens, shared):
     assert torch.equal(out[:b.total], c.expand(b.total, 8, D))
 
 
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.125, 1e-40, -1e-40])
+def test_attn_any_finite_scale(dt, D, scale):
+    """Zero weighs all seen keys alike, a negative one prefers the least
+    products; short last tiles, masks and parts among narrow and wide blocks."""
+    r = random.Random(D)
+    for rows, lens, shared in (([1, 3], [70, 5], 0), ([1, 2, 5], [600, 33, 0], 90), ([50, 34], [290, 417], 0),
+                               ([64], [300], 333)):
+        for mask in (None, bh.trie_masks(r, rows, 1)[0]):
+            b = Batch(dt, 8, 2, D, 16, rows, lens, shared=shared, mask=mask, pad=1, seed=shared)
+            b.scale = scale
+            b.check(b.attend())
+
+
 # ----------------------------------------------------------------- compact
 
 
