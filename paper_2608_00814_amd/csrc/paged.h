@@ -76,8 +76,24 @@ inline int check_paged(const char* who, const ooo_paged_batch* b, Paged& p) {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// The new rows of all sequences that the buffers hold.
+__device__ __forceinline__ int rows_of(const Paged& p) { return min(max(p.row_start[p.n_seqs], 0), p.n_rows); }
+// A sequence's rows and own tokens, bounded to what buffers and tables hold
+// (R: rows_of).
+struct Seq {
+  int row0, rows, len;
+};
+__device__ __forceinline__ Seq seq_of(const Paged& p, int b, int R) {
+  Seq s;
+  s.row0 = min(max(p.row_start[b], 0), R);
+  s.rows = min(max(p.row_start[b + 1], s.row0), R) - s.row0;
+  s.len = min(max(p.seq_len[b], 0), p.own_cap);
+  return s;
+}
+
 // The sequence of row r (0 <= r < row_start[n]): the last b with
-// row_start[b] <= r, found by the whole wave, 64 bounds at a time: one round
+// row_start[b] <= r, where row_start rises from 0 (else any, to be checked
+// against its rows), found by the whole wave, 64 bounds at a time: one round
 // trip for 64 sequences, two for 4096.  Every lane gets the answer.
 __device__ __forceinline__ int seq_of_row(const int32_t* row_start, int n, int r, int lane) {
   int lo = 0, len = n;  // the answer lies in [lo, lo + len)

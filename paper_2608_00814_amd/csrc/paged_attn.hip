@@ -15,18 +15,6 @@ namespace {
 constexpr int kPlanThreads = 512;
 
 // ------------------------------------------------------------------- plan
-// A sequence's rows and own tokens, bounded to what buffers and tables hold.
-struct Seq {
-  int row0, rows, len;
-};
-__device__ __forceinline__ Seq seq_of(const Paged& p, int b, int R) {
-  Seq s;
-  s.row0 = min(max(p.row_start[b], 0), R);
-  s.rows = min(max(p.row_start[b + 1], s.row0), R) - s.row0;
-  s.len = min(max(p.seq_len[b], 0), p.own_cap);
-  return s;
-}
-
 // Whether query rows against so many keys go to wide blocks.
 __device__ __forceinline__ bool wide_rows(const PlanShape& s, int rows, int keys) {
   return rows > s.narrow && (s.narrow == 0 || keys > kShortTiles * kTileKeys);
@@ -161,7 +149,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
   Item* const items_w = reinterpret_cast<Item*>(plan + s.off_items_w);
   Item* const items_n = reinterpret_cast<Item*>(plan + s.off_items_n);
   const int tid = threadIdx.x;
-  const int R = min(max(p.row_start[p.n_seqs], 0), p.n_rows);
+  const int R = rows_of(p);
   const int stack = R * p.G;  // query rows of a KV head
   const bool swide = wide_rows(s, stack, p.shared_len);
   const int sblock = swide ? s.wide : s.narrow;
@@ -326,7 +314,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
 // Where the parts of each query row lie.
 __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, uint8_t* plan) {
   const int x = blockIdx.x * 256 + threadIdx.x;
-  const int R = min(max(p.row_start[p.n_seqs], 0), p.n_rows);
+  const int R = rows_of(p);
   if (x >= R * p.G) return;
   const int r = x / p.G;
   int lo = 0, hi = p.n_seqs - 1;  // last b with row_start[b] <= r

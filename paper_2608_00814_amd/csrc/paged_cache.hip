@@ -65,9 +65,12 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(
   const bool on = h < nh;
   const T* src = qkv + (size_t)r * ld + (size_t)min(h, nh - 1) * D + j0;
   const u32x4 xa = ld16(src), xb = ld16(src + HALF);
-  if (r >= min(p.row_start[p.n_seqs], p.n_rows)) return;
+  const int R = rows_of(p);
+  if (r >= R) return;
   const int b = __builtin_amdgcn_readfirstlane(seq_of_row(p.row_start, p.n_seqs, r, lane));
-  const int len = p.seq_len[b], i = r - p.row_start[b];
+  const Seq q = seq_of(p, b, R);
+  const int len = p.seq_len[b], i = r - q.row0;
+  if (i < 0 || i >= q.rows) return;  // no sequence's row
   const long long slot = (long long)len + i;
   const int pos = p.shared_len + len + (depth ? depth[r] : i);
   bool ok = len >= 0 && slot < p.own_cap;

@@ -97,6 +97,28 @@ def test_append_drops_rows_without_a_page():
     assert np.isfinite(got).all()
 
 
+@pytest.mark.parametrize("starts", [[5, 9, 14], [0, 9, 4], [9, -3, 14], [-4, 9, 1 << 30]])
+def test_append_bounds_row_starts(starts):
+    """row_start that does not begin at 0 or falls: rows outside every
+    sequence's range have no place (none ahead of a page table either)."""
+    b = Batch("bf16", 2, 1, 64, 16, [9, 5], [0, 0])
+    b.d_row_start.copy_(torch.tensor(starts, dtype=torch.int32))
+    qkv = torch.randn((b.n_rows, 4 * 64), device="cuda").to(b.dt)
+    q_out = torch.full((b.n_rows, 2, 64), 7.0, dtype=b.dt, device="cuda")
+    k0, v0 = f64(b.k), f64(b.v)
+    ooo.paged_append(b.batch, qkv, None, None, 1e-6, 1e6, q_out, b.k, b.v)
+    R = min(max(starts[2], 0), b.n_rows)
+    lo = [min(max(s, 0), R) for s in starts]
+    places = set()
+    for s in range(2):
+        places |= {ob.place(b.table[s], i, 16) for i in range(min(max(starts[s + 1], lo[s]), R) - lo[s])}
+    got = {tuple(d) for d in np.argwhere((f64(b.v) != v0).any(axis=(1, 3)))}
+    assert got <= places and {tuple(d) for d in np.argwhere((f64(b.k) != k0).any(axis=(1, 3)))} <= places
+    if starts[0] == 5:  # two sequences of 4 and 5 rows behind 5 that are none's
+        assert got == places and (f64(q_out)[:5] == 7.0).all() and not (f64(q_out)[5:] == 7.0).all(axis=2).any()
+    assert (f64(q_out)[R:] == 7.0).all()
+
+
 # --------------------------------------------------------------- attention
 
 
