@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void compact_kernel(Paged p, uint8_t* __restri
   const int b = blockIdx.y, g = blockIdx.x >> 1;
   uint8_t* const pool = ((blockIdx.x & 1) ? v : k) + (long long)blockIdx.z * layer_bytes;
   const int L = accept[b];
-  const int len = p.seq_len[b], rows = p.row_start[b + 1] - p.row_start[b];
+  const int len = p.seq_len[b], rows = seq_of(p, b, rows_of(p)).rows;
   if (L < 0 || L >= path_cap || len < 0) return;
   const int sub = threadIdx.x % LPR, lr = threadIdx.x / LPR;
   const auto place = [&](int i) -> uint8_t* {  // of new row i, or null

@@ -474,6 +474,22 @@ def test_compact_leaves_bad_entries():
     assert np.array_equal(f64(b.k), want)
 
 
+def test_compact_bounds_rows():
+    """Rows past n_rows are none: entries of path that name them stay."""
+    b = Batch("bf16", 4, 2, 64, 16, [4, 4], [3, 2])
+    b.d_row_start[2] = 1 << 29
+    path = torch.tensor([[0, 2, 3, 5], [0, 2, 5, 7]], dtype=torch.int32, device="cuda")
+    acc = torch.tensor([3, 3], dtype=torch.int32, device="cuda")
+    k0 = f64(b.k)
+    ooo.paged_compact(b.batch, b.k, b.v, path, acc)
+    want = ob.compact(k0, b.row_start, b.lens, b.table, np.array([[0, 2, 3], [0, 2, 2]]), np.array([2, 1]))
+    assert np.array_equal(f64(b.k), want)
+    b.d_row_start.copy_(torch.tensor([-6, 2, 8], dtype=torch.int32))  # two rows of the first sequence are left
+    k0 = f64(b.k)
+    ooo.paged_compact(b.batch, b.k, b.v, path, acc * torch.tensor([1, -1], dtype=torch.int32, device="cuda"))
+    assert np.array_equal(f64(b.k), k0)  # row 0 stays, 2 and on are none
+
+
 # ------------------------------------------------------------------ sample
 
 
