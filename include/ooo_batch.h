@@ -51,6 +51,7 @@ extern "C" {
  *   n_rows        rows the step's buffers hold; row_start[n_seqs] <= n_rows;
  *                 n_rows * n_q_heads and n_rows * mask_words up to 2^28
  *   row_start     [n_seqs + 1] int32, non-decreasing, row_start[0] == 0
+ *                 (rows ahead of row_start[0] would be no sequence's)
  *   seq_len       [n_seqs] int32, >= 0
  *   page_table    [n_seqs][table_ld] int32
  *   shared_pages  [ceil(shared_len / page_rows)] int32 (NULL if shared_len is 0)
@@ -69,6 +70,8 @@ extern "C" {
  * What the host cannot check is bounded on the device: rows and tokens past
  * n_rows or past table_ld * page_rows are left out, and a page outside
  * [0, n_pages) is never dereferenced (each entry point says what comes then).
+ * Where row_start falls, attention gives NaN rows and the others leave out the
+ * rows that lie outside their sequence's range.
  */
 typedef struct {
   int32_t n_seqs;

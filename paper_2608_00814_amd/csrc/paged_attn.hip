@@ -160,6 +160,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
   // what an item's start and end cost, in wide tiles and in half-tiles of a wave
   const int lead_w = half_dim ? 16 : 8, lead_n = half_dim ? 6 : 3;
   __shared__ Deal deal_s;
+  __shared__ int falls_s;
+  if (tid == 0) falls_s = 0;
+  bool falls = false;
 
   long long all[3] = {0, 0, swide ? sblocks : 0};  // own wide tiles, narrow half-tiles, blocks
   for (int e0 = 0; e0 < entries; e0 += kPlanThreads) {
@@ -168,6 +171,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
     if (e < entries) {
       const Entry x = entry_of(p, s, e, lead, sblock, R);
       v[2] = x.n;
+      falls |= !x.shared && p.row_start[e - lead + 1] < p.row_start[e - lead];
       for (int j = 0; j < x.n; ++j) {
         int nq, limit, len;
         x.at(p, j, nq, limit, len);
@@ -175,16 +179,25 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
       }
     }
     scan<3>(v, t);
-    if (e >= lead && e < entries) seq_block[e - lead] = (int)(all[2] + v[2]);
+    if (e >= lead && e < entries) seq_block[e - lead] = (int)min(all[2] + v[2], s.max_blocks);
 #pragma unroll
     for (int k = 0; k < 3; ++k) all[k] += t[k];
   }
+  if (falls) falls_s = 1;
   const int wblocks = swide ? sblocks : 0;
   if (tid < 64) {
     const Deal d = deal_workers(p, s, wblocks, tiles, all[0], all[1], half_dim != 0, tid);
     if (tid == 0) deal_s = d;
   }
   __syncthreads();
+  // Sequences overlap where row_start falls, and their blocks, items and slots
+  // are more than there is room for, without bound.  Such a plan has no work and
+  // a key that fits no batch.
+  if (falls_s) {
+    head.key[0] = 0;
+    if (tid == 0) *reinterpret_cast<PlanHead*>(plan) = head;
+    return;
+  }
   const Deal d = deal_s;
   const int runs_w = max(d.own_workers, 1), runs_n = max(d.narrow_workers, 1) * max(s.waves, 1);
   const long long len_w = max((all[0] + runs_w - 1) / runs_w, 1ll), len_n = max((all[1] + runs_n - 1) / runs_n, 1ll);

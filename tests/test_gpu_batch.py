@@ -437,6 +437,32 @@ def test_attn_any_finite_scale(dt, D, scale):
             b.check(b.attend())
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("shared", [0, 40])
+def test_attn_row_starts_that_fall_are_visible(dt, shared):
+    """Sequences that would overlap: NaN rows, and a plan of no work."""
+    b = Batch(dt, 4, 2, 64, 16, [30, 5, 1], [40, 9, 70], shared=shared, pad=2)
+    good = b.attend()
+    for starts in ([0, 30, 10, 36], [36, 0, 36, 36], [3, 30, 29, 36]):
+        b.d_row_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        out = b.attend()
+        assert out[:36].isnan().all() and (out[36:] == 7.0).all()
+    b.d_row_start.copy_(torch.tensor([0, 30, 35, 36], dtype=torch.int32))
+    assert torch.equal(b.attend(), good)
+
+
+def test_attn_row_starts_past_the_buffers():
+    """Cut to n_rows; rows ahead of row_start[0] are no sequence's and stay as
+    they are."""
+    b = Batch("bf16", 4, 2, 64, 16, [30, 5, 1], [40, 9, 70])
+    good = b.attend()
+    b.d_row_start.copy_(torch.tensor([0, 30, 35, 1 << 30], dtype=torch.int32))
+    assert torch.equal(b.attend(), good)
+    b.d_row_start.copy_(torch.tensor([3, 30, 35, 36], dtype=torch.int32))
+    out = b.attend()
+    assert (out[:3] == 7.0).all() and torch.equal(out[30:], good[30:]) and out[3:30].isfinite().all()
+
+
 # ----------------------------------------------------------------- compact
 
 
