@@ -618,15 +618,19 @@ class PagedBatch:
 
 
 def _stream_on(device, stream) -> Optional[int]:
-    """The stream of a call on ``device``: the given one, or the device's current one."""
-    if stream is not None:
-        return _stream(stream)
+    """The stream of a call on ``device``, which has to be the current one (a
+    launch goes to that): the given stream, or the device's current one."""
     import torch
 
     current = torch._C._cuda_getDevice()
     if device.index != current:
         raise ValueError(f"the tensors are on {device}, the current device is cuda:{current}")
-    return torch._C._cuda_getCurrentRawStream(current)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(current)
+    on = getattr(stream, "device", device)
+    if on != device:
+        raise ValueError(f"the tensors are on {device}, the stream is on {on}")
+    return _stream(stream)
 
 
 def paged_append(batch: PagedBatch, qkv, q_norm, k_norm, eps: float, rope_theta: float, q_out, k_pages, v_pages,

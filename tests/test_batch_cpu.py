@@ -122,6 +122,24 @@ def test_attn_refuses_scales_that_are_not_finite(scale):
         assert "scale" in ooo.last_error()
 
 
+def test_calls_are_for_the_current_device(monkeypatch):
+    import torch
+
+    class Stream:
+        def __init__(self, device):
+            self.device, self.cuda_stream = torch.device(device), 77
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 100 + d, raising=False)
+    on = lambda d, s: ooo._stream_on(torch.device("cuda", d), s)  # noqa: E731
+    assert on(1, None) == 101 and on(1, 5) == 5 and on(1, Stream("cuda:1")) == 77
+    for s in (None, 5, Stream("cuda:0"), Stream("cuda:1")):
+        with pytest.raises(ValueError, match="current device"):
+            on(0, s)
+    with pytest.raises(ValueError, match="the stream is on"):
+        on(1, Stream("cuda:0"))
+
+
 def test_size_queries_follow_sizes_alone():
     """More rows, sequences or shared tokens never need less."""
     L = ooo.lib()
