@@ -611,6 +611,45 @@ def test_sample_counts_above_the_least_floors(V):
         run_sample(x, T=[T] * 7, p=[0.9] * 7, m=[m] * 7, u=[0.0, 0.9, 0.5, 0.3, 0.999, 0.7, 0.1])
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [300, 3000, 40000])
+def test_sample_odd_rows_of_every_length(V, dt):
+    """Rows of nothing that can be drawn, of infinite logits (more than are
+    gathered, too) and of few finite ones, in one workgroup and over many; a
+    temperature that is NaN is none."""
+    r = np.random.default_rng(V)
+    inf, nan = np.inf, np.nan
+    x = r.normal(0, 3, (10, V)).astype(np.float32)
+    x[0], x[1] = -inf, nan
+    x[2] = np.where(r.random(V) < 0.5, nan, -inf)
+    x[3, ::5] = nan
+    x[3, V // 2] = inf
+    x[4, [0, V // 3, V - 1]] = inf
+    x[5, ::2] = inf
+    x[6] = inf
+    x[7] = np.where(r.random(V) < 0.5, nan, -inf)
+    x[7, V - 2] = -3.0e38
+    x[8] = np.where(r.random(V) < 0.1, nan, np.where(r.random(V) < 0.1, -inf, x[8]))
+    x[9] = np.where(r.random(V) < 0.2, inf, np.where(r.random(V) < 0.2, nan, -inf))
+    u = [0.0, 0.5, 0.5, 0.9, 0.7, 0.6, 0.9999999, 0.3, 0.8, 0.4]
+    for k in (0, 1, 7, 600):
+        run_sample(x, k=[k] * 10, u=u, dt=dt)
+        run_sample(x, T=[0.7] * 10, k=[k] * 10, p=[0.7] * 10, m=[0.1] * 10, u=u, dt=dt)
+    run_sample(x, p=[0.9] * 10, u=u, dt=dt)
+    run_sample(x, m=[0.05] * 10, u=u, dt=dt)
+    run_sample(x, T=[nan] * 10, k=[7] * 10, p=[0.5] * 10, u=u, dt=dt)
+    run_sample(x, T=[0.0, -1.0] * 5, u=u, dt=dt)
+
+
+@pytest.mark.parametrize("V", [20011, 151936])
+@pytest.mark.parametrize("std,T", [(0.3, 1.0), (1.0, 1.0), (0.5, 0.7)])
+def test_sample_flat_logits(V, std, T):
+    """Different logits so close together that the bins with the places of
+    top-p and the draw hold more tokens than are gathered."""
+    x = np.random.default_rng(V).normal(0, std, (4, V)).astype(np.float32)
+    run_sample(x, T=[T] * 4, p=[0.9, 0.5, 1.0, 0.95], m=[0.0, 0.0, 0.05, 0.2], u=[0.9, 0.3, 0.7, 0.05])
+
+
 # ---------------------------------------------------------------- together
 
 
