@@ -477,7 +477,7 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
     f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < KS; ++dt) zero += o[dt] * 0.f;
-    const int odd = __any(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f));
+    const int odd = __any(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f) && l_run < INFINITY);
     if (lane == 0) odd_s[wave] = (odd ? 1 : 0) | (__any(bad) ? 2 : 0);
     __syncthreads();
     float m = -INFINITY, den = 0.f;
@@ -486,9 +486,10 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
     const bool poison = __any(lane < NW && (odd_s[lane < NW ? lane : 0] & 2));
     // A value of V that is not finite counts only for the query rows that give
     // its key a weight, but the matrix products multiply it by the zeros of the
-    // others too, and zero times it is NaN.  So where a wave's sums are not
-    // finite the block adds its keys once more, one by one and relative to the
-    // rows' final exponents, without those of weight zero.
+    // others too, and zero times it is NaN.  So where a wave has a row of such
+    // sums the block adds its keys once more, one by one and relative to the
+    // rows' final exponents, without those of weight zero.  (Not for a row whose
+    // weights are not finite: that is NaN either way.)
     if (__any(lane < NW && (odd_s[lane < NW ? lane : 0] & 1))) {
       __syncthreads();  // every wave has read ml_s and odd_s
       l_run = 0.f;

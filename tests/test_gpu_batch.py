@@ -463,6 +463,39 @@ def test_attn_row_starts_past_the_buffers():
     assert (out[:3] == 7.0).all() and torch.equal(out[30:], good[30:]) and out[3:30].isfinite().all()
 
 
+def batch_us(b, plan, ws, out):
+    """Least of ten calls."""
+    e = [torch.cuda.Event(enable_timing=True) for _ in range(11)]
+    for x in e:
+        x.record()
+        ooo.paged_attn(b.batch, plan, b.q, b.k, b.v, b.scale, out, ws)
+    torch.cuda.synchronize()
+    return 1e3 * min(x.elapsed_time(y) for x, y in zip(e, e[1:]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_attn_bad_queries_stay_their_own(dt, rows):
+    """Queries and keys that are not finite: NaN rows for their sequence, the
+    same bits for the others, and no second pass over the shared keys (40 times
+    the batch's time; 4 leaves room for noise)."""
+    n = 40 // rows
+    b = Batch(dt, 8, 2, 128, 16, [rows] * n, [50] * n, shared=2000, pad=1, seed=rows)
+    plan, out = ooo.paged_plan(b.batch), torch.full_like(b.q, 7.0)
+    ws = torch.empty(ooo.paged_attn_workspace(b.batch), dtype=torch.uint8, device="cuda")
+    good, before = b.attend(), batch_us(b, plan, ws, out)
+    b.q[rows:2 * rows, 3, 5] = float("nan")      # a query head of sequence 1
+    b.q[0, 1] = float("inf")
+    pg, sl = ob.place(b.table[n - 1], 7, 16)
+    b.k[pg, 1, sl] = float("nan")                # a key of the last sequence's second KV head
+    after = batch_us(b, plan, ws, out)
+    bad = torch.zeros(b.n_rows, 8, dtype=torch.bool, device="cuda")
+    bad[rows:2 * rows, 3] = bad[0, 1] = True
+    bad[b.total - rows:b.total, 4:] = True
+    assert out[bad].isnan().all() and torch.equal(out[~bad], good[~bad])
+    assert after < 4 * before, (before, after)
+
+
 # ----------------------------------------------------------------- compact
 
 
