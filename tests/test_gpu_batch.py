@@ -683,6 +683,44 @@ def test_sample_flat_logits(V, std, T):
     run_sample(x, T=[T] * 4, p=[0.9, 0.5, 1.0, 0.95], m=[0.0, 0.0, 0.05, 0.2], u=[0.9, 0.3, 0.7, 0.05])
 
 
+@pytest.mark.parametrize("V", [3000, 70000])
+def test_sample_captured_and_replayed(V):
+    """Two captured draws with settings of their own on two streams, replayed
+    over new logits and numbers: the ids, probabilities and counts of a call."""
+    f, i = torch.float32, torch.int32
+    sets = [dict(temperature=torch.full((5,), 0.8, device="cuda"), top_k=torch.tensor([0, 1, 40, 600, 0], dtype=i, device="cuda"),
+                 top_p=torch.tensor([0.9, 1.0, 0.8, 0.7, 1.0], device="cuda")),
+            dict(min_p=torch.full((5,), 0.05, device="cuda"))]
+    runs = []
+    for kw in sets:
+        t = {"x": torch.randn(5, V, device="cuda") * 3, "u": torch.rand(5, device="cuda"),
+             "ids": torch.zeros(5, dtype=i, device="cuda"), "prob": torch.zeros(5, dtype=f, device="cuda"),
+             "kept": torch.zeros(5, dtype=i, device="cuda"),
+             "ws": torch.zeros(ooo.sample_workspace(5, V), dtype=torch.uint8, device="cuda")}
+        call = lambda t, kw=kw: ooo.sample(t["x"], t["u"], t["ids"], t["ws"], prob=t["prob"], kept=t["kept"], **kw)  # noqa: E731
+        call(t)
+        torch.cuda.synchronize()
+        s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call(t)
+        runs.append((t, call, s, g))
+    for step in range(4):
+        for t, *_ in runs:
+            t["x"].normal_(0, 3 - 0.7 * step)
+            t["u"].uniform_()
+            t["ws"].fill_(0xFF)
+        torch.cuda.synchronize()
+        for _, _, s, g in runs:
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for t, call, *_ in runs:
+            got = [t[n].clone() for n in ("ids", "prob", "kept")]
+            call(t)
+            assert all(torch.equal(a, t[n]) for a, n in zip(got, ("ids", "prob", "kept")))
+            assert (t["ids"] >= 0).all()
+
+
 # ---------------------------------------------------------------- together
 
 
@@ -775,3 +813,28 @@ def test_steps_captured_and_replayed(dt):
         for b in (a, e):
             b.lens = [n + int(c) + 1 for n, c in zip(b.lens, acc)]
         assert a.d_len.tolist() == a.lens
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_layers_interleaved_in_one_pool(dt):
+    """Pages that hold the rows of three layers: one layer's calls and a
+    compaction of all of them leave the others' rows alone."""
+    r = random.Random(8)
+    rows, lens = [20, 3, 9], [25, 60, 7]
+    mask, depth = bh.trie_masks(r, rows, 1)
+    b = Batch(dt, 4, 2, 64, 16, rows, lens, shared=21, mask=mask, seed=6)
+    n, Hkv, R, D = b.k.shape
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((n, 3, Hkv, R, D), generator=g, device="cuda").to(b.dt).transpose(0, 1) for _ in range(2))
+    b.k, b.v = k[1], v[1]
+    b.batch = ooo.PagedBatch(b.d_row_start, b.d_len, b.d_table, b.k, 4, b.n_rows, shared_pages=b.d_shared,
+                             shared_len=21, anc_mask=b.d_mask)
+    others = [f64(t[i]) for t in (k, v) for i in (0, 2)]
+    run_append(b, True, depth)
+    b.check(b.attend())
+    assert all(np.array_equal(a, f64(t)) for a, t in zip(others, [t[i] for t in (k, v) for i in (0, 2)]))
+    path, acc = np.full((3, 20), -1, np.int32), np.array([4, -1, 2], np.int32)
+    path[0, :5], path[2, :3] = [0, 3, 8, 9, 19], [0, 1, 7]
+    want = [np.stack([ob.compact(f64(t[i]), b.row_start, lens, b.table, path, acc) for i in range(3)]) for t in (k, v)]
+    ooo.paged_compact(b.batch, k, v, torch.from_numpy(path).cuda(), torch.from_numpy(acc).cuda())
+    assert np.array_equal(f64(k), want[0]) and np.array_equal(f64(v), want[1])
