@@ -153,7 +153,9 @@ int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, 
  * A row that sees no key at all is zero.  A key that a row does not see has
  * no influence on it, whatever its k and v hold (NaN and infinities too).  A
  * page outside [0, n_pages) where keys are read gives NaN rows to those who
- * read it (a shared page: to all).
+ * read it (a shared page: to all), and to rows of the same sequence that are
+ * worked on together with them (up to 128 query rows of a KV head) though they
+ * do not see its keys.
  * Errors: as for ooo_paged_append; OOO_ERR_CAPACITY (ws_bytes, plan_bytes).
  */
 size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch);

@@ -137,9 +137,14 @@ __device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int
   return best;
 }
 
-// One workgroup, 15 to 30 us for up to 256 sequences, once a step.  First the
-// lengths, from them the deal, then the items and slots of every entry behind
-// those of the entries before it.
+// One workgroup, once a step.  First the lengths, from them the deal, then the
+// items and slots of every entry behind those of the entries before it.  A
+// sequence is one thread's work, block by block, so the time grows with the
+// blocks of the longest one, 1.4 us each.  With plan_rows_kernel (4 to 6 us): 16
+// us for 64 sequences of a row, 18 for 256, 75 for 4096; 19 for 8 of 64 rows of
+// four query heads a group, 59 for one of 1024, 190 for one of 4096 and 695 for
+// one of 16384 (128 wide blocks in 4096 rows); in float32, whose blocks are an
+// eighth of that, 36 for 3 of 25 rows, 190 for one of 512, 1370 for one of 4096.
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, int half_dim,
                                                             uint8_t* plan) {
   BlockSlots* const blocks = reinterpret_cast<BlockSlots*>(plan + s.off_blocks);
@@ -565,9 +570,10 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
 // head and the row's slots are asked for together, then four slots at a time:
 // 5 us for 64 rows of 32 heads, 7 for 385.  Few rows may be split over hundreds
 // of slots; then four waves share a piece's (PAR), eight slots at a time each:
-// the call for two rows over a 22k prompt takes 51 us, 130 with one.  More rows
-// have few parts, and four times the waves cost more: 60 us, not 47, for 1145
-// rows of four prompts.  Hence the bound on the workgroups in launch_attn.
+// the call for one row of 32 heads over a 22k prompt takes 42 us, 120 with one,
+// for two rows 33 and 94.  More rows have few parts, and four times the waves
+// cost more: 56 us, not 44, for 1145 rows of four prompts.  Hence the bound on
+// the workgroups in launch_attn.
 template <class T, int D, int PAR>
 __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
   constexpr bool BF = sizeof(T) == 2;

@@ -12,7 +12,7 @@
 //    each with one 32-key half of every tile.  K and V tiles go through two
 //    rings of four stages that all waves fill and read.  A SIMD holds one wave
 //    of either half, and a tile costs them 1024 cycles of matrix products, about
-//    1200 of vector work (512 of it exponentials) and 1070 of LDS traffic; at
+//    1130 of vector work (512 of it exponentials) and 1070 of LDS traffic; at
 //    two waves a SIMD (the accumulators leave no room for more) they overlap to
 //    2100 cycles a tile, against 2650 with each wave's products, reads, copies
 //    and vector work behind one another.
@@ -21,7 +21,10 @@
 //    and the end of one wave's items lie under the streams of the others.  A
 //    half-tile's K is read into registers whole, so the next one's is on its
 //    way while it is used, and V likewise: 16 KiB (head_dim 128) a wave.
-//    Bound by HBM: 256 sequences of 1.2 GB in 225 us on half of the CUs, 5.3 TB/s.
+//    Bound by HBM: one row of 256 sequences with 2049 keys each, 2.1 GB, in 326
+//    us, 6.6 TB/s.  Beside the wide items of a 32k prompt a worker's waves 4 to 7,
+//    the younger ones of their SIMDs, end at 282 us where waves 0 to 3, with as
+//    many half-tiles, end at 217.
 // Rows of a tile are copied by LDS DMA, 4 or 8 at a time, which never cross a
 // page (pages hold a multiple of 16 rows).
 #pragma once

@@ -42,10 +42,10 @@ constexpr int kTileKeys = 64;
 constexpr int kShortTiles = 4;
 constexpr int kSplitMost = 4;  // extra items of the shared blocks: at most so many times the workers
 
-// Waves of a float32 worker, and workers on a CU at once (the kernel keeps 168
-// registers at head_dim 64 and 248 at 128; forced to 168, it spills and takes
-// twice the time, and eight waves a worker, one of which fills a CU, take 10%
-// longer).
+// Waves of a float32 worker, and workers on a CU at once (the kernel keeps 148
+// registers at head_dim 64 and 249 at 128; at 128 forced to 168, it spills and
+// takes twice the time, and eight waves a worker, one of which fills a CU, take
+// 10% longer).
 constexpr int kF32Waves = 4;
 __host__ __device__ constexpr int f32_per_cu(int head_dim) { return head_dim == 64 ? 3 : 2; }
 

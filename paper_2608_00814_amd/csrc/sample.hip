@@ -21,8 +21,10 @@
 //
 // Rows of up to kOneBlock tokens are one workgroup's work: one launch, where
 // chunks take four (240 rows of 11053: 24 us, 46 in chunks; 17 rows of 17940:
-// 27 and 34; 28 rows of 30630: 39 and 36).  Longer ones are cut into chunks
-// over many workgroups.  The first launch finds the largest
+// 27 and 34).  Near the bound it depends on the settings and the rows: of 32000
+// tokens, 1, 28 and 100 rows with top-k 50 take 11, 12 and 13 us, and 16, 18 and
+// 25 in chunks; with top-p alone 33, 35 and 35, and 25, 30 and 48.  Longer ones
+// are cut into chunks over many workgroups.  The first launch finds the largest
 // logit and those of up to kGroups disjoint groups of tokens.
 //  * With top-k (or greedily), no token below the k-th largest of the groups'
 //    largest logits can be kept, and only the groups that reach that are read
@@ -30,6 +32,12 @@
 //    more than k, sorts them and answers from them alone.
 //  * Other rows need the two launches between: the histogram and the
 //    gathering; they come from HBM once and from the last-level cache twice.
+// Where the bins that are needed hold more than kGather tokens, one workgroup
+// finds the places digit by digit over the whole row, up to eighteen passes.
+// Many equal logits do that, and so do flat ones: a bin is 0.0156 T wide, and of
+// 151936 normal logits with standard deviation 1, T 1 and top-p 0.9 without
+// top-k more lie in them.  That row takes 1.3 ms (25 to 50 us with a standard
+// deviation of 2.5 to 1.28), 64 such rows 1.5 and 256 rows 2.1.
 // (Left to the last workgroup of a row to finish, the answers cost more than
 // their launch: each workgroup's release and acquire across the XCDs' caches
 // took 256 rows of 152064 from 183 to 255 us.)
@@ -556,7 +564,7 @@ struct Found {
 
 // The place of the row at which the running count or weight exceeds `target`,
 // found digit by digit over the keys: four passes over the row.  For rows
-// whose close bins hold more than fits (many equal logits).
+// whose close bins hold more than fits (many equal logits, or flat ones).
 template <class T, int NT>
 __device__ Found radix_find(const T* x, int V, const Row& s, bool by_weight, u64 target, u64* hw, u64* hc) {
   static_assert(NT >= 256, "a digit a thread");
