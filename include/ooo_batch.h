@@ -156,7 +156,8 @@ int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, 
  * read it (a shared page: to all), and to rows of the same sequence that are
  * worked on together with them (up to 128 query rows of a KV head) though they
  * do not see its keys.
- * Errors: as for ooo_paged_append; OOO_ERR_CAPACITY (ws_bytes, plan_bytes).
+ * Errors: as for ooo_paged_append; OOO_ERR_INVALID (a scale that is not finite),
+ * OOO_ERR_CAPACITY (ws_bytes, plan_bytes).
  */
 size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch);
 int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_bytes, const void* q,
