@@ -22,7 +22,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libooo.so")
 
 HIP_SOURCES = ["tree_attn.hip", "lmhead.hip", "accept_compact.hip", "layer.hip", "linear.hip", "paged_cache.hip",
-               "paged_attn.hip", "sample.hip"]
+               "paged_attn.hip", "cache8.hip", "sample.hip"]
 HOST_SOURCES = ["host.cpp"]
 ARCH = "gfx950"
 

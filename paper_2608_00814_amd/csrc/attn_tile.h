@@ -13,6 +13,7 @@ constexpr int kTile = 64;  // keys of a tile
 __device__ __forceinline__ int sigma(int c) { return (c & ~0xC) | ((c & 4) << 1) | ((c & 8) >> 1); }
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 // Kernel-local lambdas must be inlined: an outlined call would take its
 // captures through memory and lose their wave-uniformity (the DMA needs
 // scalar operands).

@@ -2,6 +2,7 @@
 // keys that a row sees and an item's pages.
 #pragma once
 
+#include "cache8.h"
 #include "paged_plan.h"
 
 namespace ooo {
@@ -20,6 +21,7 @@ struct PagedAttnArgs {
   float* part_ml;       // [slot][Hkv][group] (m, l)
   long long max_slots;
   float scale_log2e;    // bf16: its size
+  Cache8 c;             // of 8-bit pages
 };
 
 // Memory that no kernel writes while it is read here, the same address in the

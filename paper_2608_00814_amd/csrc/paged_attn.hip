@@ -7,6 +7,7 @@
 // outputs O: O = sum_s exp2(m_s - m) O_s / sum_s exp2(m_s - m) l_s.  That is
 // what lets the shared prompt be read once, for the stacked rows of all
 // sequences, and long sequences be split.  Parts and statistics are float32.
+#include "paged_attn8.h"
 #include "paged_attn_bf16.h"
 
 namespace ooo {
@@ -86,22 +87,19 @@ __device__ __forceinline__ void scan(long long (&v)[N], long long (&total)[N]) {
 struct Deal {
   int splits, shared_workers, own_workers, narrow_workers;
 };
-// Costs in 100 cycles at head_dim 128 (half of them at 64), as measured: a wide
-// tile of a worker; an item's start (its record, pages, queries and first
-// tiles, one behind the other) and end; a half-tile of a narrow worker, whose
-// eight waves have 128 KiB on their way; and a half-tile at the chip's share of
-// the HBM rate.
-constexpr float kCostTile = 21.f, kCostItem = 160.f, kCostHalf = 5.f, kCostHalfHbm = 0.05f;
+constexpr PlanCosts kCosts{21.f, 160.f, 5.f, 0.05f};
+// 8-bit pages: half the bytes of a half-tile.
+constexpr PlanCosts kCosts8{24.f, 160.f, 2.5f, 0.025f};
 
 // The deal that finishes first, for every lane of a wave, each of which tries
 // its share of the split counts (one lane alone took 40 us for 65 of them).
 // blocks, tiles: of the wide shared part; own: tiles of the sequences' wide
 // blocks; halves: of the narrow blocks.
-__device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int tiles, long long own,
-                             long long halves, bool half_dim, int lane) {
+__device__ Deal deal_workers(const Paged& p, const PlanShape& s, const PlanCosts& cost, int blocks, int tiles,
+                             long long own, long long halves, bool half_dim, int lane) {
   const int W = s.workers;
-  const float tile = half_dim ? 0.5f * kCostTile : kCostTile, half = half_dim ? 0.5f * kCostHalf : kCostHalf;
-  const float hbm = (half_dim ? 0.5f : 1.f) * kCostHalfHbm * p.Hkv * (float)halves;
+  const float tile = half_dim ? 0.5f * cost.tile : cost.tile, half = half_dim ? 0.5f * cost.half : cost.half;
+  const float hbm = (half_dim ? 0.5f : 1.f) * cost.half_hbm * p.Hkv * (float)halves;
   Deal best{1, 0, 0, 0};
   float least = INFINITY;
   const int kinds = (blocks > 0) + (own > 0) + (halves > 0);
@@ -122,8 +120,8 @@ __device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int
         wo = min(max(wo, 1), rest - 1);
         wn = rest - wo;
       }
-      float t = blocks > 0 ? k * ((float)((tiles + n - 1) / n) * tile + kCostItem) : 0.f;
-      if (wo > 0) t = fmaxf(t, co / wo + kCostItem);
+      float t = blocks > 0 ? k * ((float)((tiles + n - 1) / n) * tile + cost.item) : 0.f;
+      if (wo > 0) t = fmaxf(t, co / wo + cost.item);
       if (wn > 0) t = fmaxf(t, fmaxf(cn / wn, hbm));
       if (t < least) least = t, best = Deal{n, ws, wo, wn};
     }
@@ -145,8 +143,8 @@ __device__ Deal deal_workers(const Paged& p, const PlanShape& s, int blocks, int
 // four query heads a group, 59 for one of 1024, 190 for one of 4096 and 695 for
 // one of 16384 (128 wide blocks in 4096 rows); in float32, whose blocks are an
 // eighth of that, 36 for 3 of 25 rows, 190 for one of 512, 1370 for one of 4096.
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanHead head, int half_dim,
-                                                            uint8_t* plan) {
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s, PlanCosts cost, PlanHead head,
+                                                            int half_dim, uint8_t* plan) {
   BlockSlots* const blocks = reinterpret_cast<BlockSlots*>(plan + s.off_blocks);
   int* const seq_block = reinterpret_cast<int*>(plan + s.off_seqs);
   int* const first_w = reinterpret_cast<int*>(plan + s.off_first_w);
@@ -191,7 +189,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(Paged p, PlanShape s
   if (falls) falls_s = 1;
   const int wblocks = swide ? sblocks : 0;
   if (tid < 64) {
-    const Deal d = deal_workers(p, s, wblocks, tiles, all[0], all[1], half_dim != 0, tid);
+    const Deal d = deal_workers(p, s, cost, wblocks, tiles, all[0], all[1], half_dim != 0, tid);
     if (tid == 0) deal_s = d;
   }
   __syncthreads();
@@ -363,6 +361,30 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(Paged p, PlanShape s, ui
 // ------------------------------------------------------ attention, float32
 __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
+// Keys and values in float32, and in 8 bits with a scale for the 16 rows of a
+// tile: four elements as they are read, and as numbers.
+struct Rows32 {
+  using T = float;
+  using Raw = f32x4;
+  static __device__ __forceinline__ Raw read(const T* p) { return load4(p); }
+  static __device__ __forceinline__ f32x4 get(Raw x, float) { return x; }
+  static __device__ __forceinline__ float scale(const PagedAttnArgs&, int, int, int, int) { return 1.f; }
+};
+struct Rows8 {
+  using T = uint8_t;
+  using Raw = uint32_t;
+  static __device__ __forceinline__ Raw read(const T* p) { return *reinterpret_cast<const uint32_t*>(p); }
+  static __device__ __forceinline__ f32x4 get(Raw x, float up) {
+    float f[4];
+    values4(x, up, f);
+    return f32x4{f[0], f[1], f[2], f[3]};
+  }
+  static __device__ __forceinline__ float scale(const PagedAttnArgs& a, int kv, int page, int g, int row) {
+    return scale_of(a.c.scales[kv] + (long long)page * a.c.scale_stride + (long long)g * a.c.page_blocks +
+                    row / kBlockRows);
+  }
+};
+
 // One item of up to 16 query rows on the f32 matrix instruction (16x16x4).
 // The keys go in tiles of 16, dealt round-robin to the waves; a wave computes
 // S^T = K Q^T and O^T += V^T P^T with its own online softmax, and the waves
@@ -372,7 +394,7 @@ __device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cas
 // of the O^T accumulator dt holds row c, columns 64 (dt / 4) + 16 q + 4 r +
 // dt % 4.  Bound by latency where it is used (float32 is the small option): 53
 // rows of three tries over 128 + 100 tokens take 6.3 us.
-template <int D>
+template <int D, class C>
 __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_kernel(PagedAttnArgs a) {
   constexpr int NW = kF32Waves;
   constexpr int KS = D / 16;
@@ -392,24 +414,29 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
     const long long row = (long long)it.row0 + i;
     const Pages pages(p, it);
     const int head_off = g << p.page_shift, in_page = (1 << p.page_shift) - 1;
-    const float* const kp = (const float*)a.k;
-    const float* const vp = (const float*)a.v;
+    using T = typename C::T;
+    const T* const kp = (const T*)a.k;
+    const T* const vp = (const T*)a.v;
     const int s0 = 4 * it.t0, s1 = min(4 * it.t1, (it.limit + 15) / 16);
     const int all = all_see(p, it);
     bool bad = false;
 
-    f32x4 qv[KS], kv[KS];
+    f32x4 qv[KS];
+    typename C::Raw kv[KS];
+    float k_up = 1.f;
     const float* const qrow = (const float*)a.q + (row * p.Hq + head_q) * D + 4 * qd;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qv[s] = load4(qrow + 16 * s) * a.scale_log2e;
     // rows past the keys re-read the last one (weight zero)
-    const auto tile_base = [&](int t) {
-      return (long long)pages.at(16 * t, bad) * p.page_stride + ((long long)head_off + ((16 * t) & in_page)) * D;
+    const auto tile_base = [&](int page, int t) {
+      return (long long)page * p.page_stride + ((long long)head_off + ((16 * t) & in_page)) * D;
     };
     const auto load_k = [&](int t) {
-      const float* kr = kp + tile_base(t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
+      const int page = pages.at(16 * t, bad);
+      const T* kr = kp + tile_base(page, t) + (size_t)min(c, it.limit - 1 - 16 * t) * D + 4 * qd;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) kv[s] = load4(kr + 16 * s);
+      for (int s = 0; s < KS; ++s) kv[s] = C::read(kr + 16 * s);
+      k_up = C::scale(a, 0, page, g, (16 * t) & in_page);
     };
     f32x4 o[KS];
 #pragma unroll
@@ -418,18 +445,22 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
     if (s0 + wave < s1) load_k(s0 + wave);
     for (int t = s0 + wave; t < s1; t += NW) {
       const int lo = 16 * t;
-      f32x4 vv[4][D / 64];
-      const float* const vb = vp + tile_base(t);
+      typename C::Raw vv[4][D / 64];
+      const int page = pages.at(16 * t, bad);
+      const T* const vb = vp + tile_base(page, t);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int h = 0; h < D / 64; ++h)
-          vv[r][h] = load4(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
+          vv[r][h] = C::read(vb + (size_t)min(4 * qd + r, it.limit - 1 - lo) * D + 64 * h + 4 * c);
+      const float v_up = C::scale(a, 1, page, g, (16 * t) & in_page);
       f32x4 score = {0.f, 0.f, 0.f, 0.f};
       // chains of eight products added in a tree: few roundings in a row
 #pragma unroll
       for (int s = 0; s < KS; s += 4) {
-        f32x4 sc[8];
+        f32x4 sc[8], kk[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) kk[x] = C::get(kv[s + x], k_up);
 #pragma unroll
         for (int ch = 0; ch < 8; ++ch) sc[ch] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -437,7 +468,7 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
 #pragma unroll
           for (int ch = 0; ch < 8; ++ch) {
             const int x = s + ch / 2, e = 2 * (ch & 1) + j;
-            sc[ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[x][e], qv[x][e], sc[ch], 0, 0, 0);
+            sc[ch] = __builtin_amdgcn_mfma_f32_16x16x4f32(kk[x - s][e], qv[x][e], sc[ch], 0, 0, 0);
           }
         score += ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
       }
@@ -465,12 +496,17 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
 #pragma unroll
       for (int r = 0; r < 4; ++r) pr[r] = exp2f(pr[r] - base);
       l_run += (pr[0] + pr[1]) + (pr[2] + pr[3]);
+      f32x4 vn[4][D / 64];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) vn[r][h] = C::get(vv[r][h], v_up);
 #pragma unroll
       for (int dt = 0; dt < KS; ++dt) {
         f32x4 pv[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          pv[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[r][dt >> 2][dt & 3], pr[r], pv[r & 1], 0, 0, 0);
+          pv[r & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vn[r][dt >> 2][dt & 3], pr[r], pv[r & 1], 0, 0, 0);
         o[dt] += pv[0] + pv[1];
       }
     }
@@ -502,26 +538,28 @@ __global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_
       for (int dt = 0; dt < KS; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
       for (int t = s0 + wave; t < s1; t += NW) {
         const int lo = 16 * t;
-        const long long tb = tile_base(t);
+        const int page = pages.at(lo, bad);
+        const long long tb = tile_base(page, t);
+        const float ku = C::scale(a, 0, page, g, lo & in_page), vu = C::scale(a, 1, page, g, lo & in_page);
         const uint64_t mw = seen(p, it, i, (int)row, lo);
 #pragma unroll 1
         for (int j = 0; j < 16 && lo + j < it.limit; ++j) {
-          const float* kr = kp + tb + (size_t)j * D + 4 * qd;
+          const T* kr = kp + tb + (size_t)j * D + 4 * qd;
           f32x4 s4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int s = 0; s < KS; ++s) s4 += load4(kr + 16 * s) * (load4(qrow + 16 * s) * a.scale_log2e);
+          for (int s = 0; s < KS; ++s) s4 += C::get(C::read(kr + 16 * s), ku) * (load4(qrow + 16 * s) * a.scale_log2e);
           float sc = (s4[0] + s4[1]) + (s4[2] + s4[3]);
           sc += shfl_xor_f(sc, 16);
           sc += shfl_xor_f(sc, 32);
           const float pk = (mw >> j) & 1ull ? exp2f(sc - base) : 0.f;
           if (pk == 0.f) continue;
           l_run += pk;
-          const float* vr = vp + tb + (size_t)j * D + 16 * qd;
+          const T* vr = vp + tb + (size_t)j * D + 16 * qd;
 #pragma unroll
           for (int h = 0; h < D / 64; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const f32x4 x = load4(vr + 64 * h + 4 * e);
+              const f32x4 x = C::get(C::read(vr + 64 * h + 4 * e), vu);
 #pragma unroll
               for (int d4 = 0; d4 < 4; ++d4) o[4 * h + d4][e] += pk * x[d4];
             }
@@ -657,13 +695,16 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
 }
 
 template <class T, int D>
-void launch_attn(const PagedAttnArgs& a, const PlanShape& s, bool neg, hipStream_t st) {
+void launch_attn(const PagedAttnArgs& a, const PlanShape& s, bool eight, bool neg, hipStream_t st) {
   const unsigned items = (unsigned)(s.workers * a.p.Hkv);
   if constexpr (sizeof(T) == 2) {
-    if (neg) paged_attn_bf16_kernel<D, true><<<items, 64 * kPagedWaves, 0, st>>>(a);
+    if (eight && neg) paged_attn8_kernel<D, true><<<items, 64 * kPagedWaves, 0, st>>>(a);
+    else if (eight) paged_attn8_kernel<D, false><<<items, 64 * kPagedWaves, 0, st>>>(a);
+    else if (neg) paged_attn_bf16_kernel<D, true><<<items, 64 * kPagedWaves, 0, st>>>(a);
     else paged_attn_bf16_kernel<D, false><<<items, 64 * kPagedWaves, 0, st>>>(a);
   } else {
-    paged_attn_f32_kernel<D><<<items, 64 * kF32Waves, 0, st>>>(a);
+    if (eight) paged_attn_f32_kernel<D, Rows8><<<items, 64 * kF32Waves, 0, st>>>(a);
+    else paged_attn_f32_kernel<D, Rows32><<<items, 64 * kF32Waves, 0, st>>>(a);
   }
   const long long groups = ((long long)a.p.n_rows * a.p.G + s.group - 1) / s.group;
   const long long blocks = groups * a.p.Hkv * (D * s.group / 1024);
@@ -675,65 +716,45 @@ size_t workspace_bytes(const ooo_paged_batch& b, const PlanShape& s) {
   return (size_t)s.max_slots * b.n_kv_heads * s.group * (b.head_dim + 2) * sizeof(float);
 }
 
-}  // namespace
-}  // namespace ooo
-
-using namespace ooo;
-
-extern "C" size_t ooo_paged_plan_bytes(const ooo_paged_batch* batch) {
-  Paged p{};
-  if (check_paged("ooo_paged_plan_bytes", batch, p) != OOO_OK) return 0;
-  return (size_t)plan_shape(*batch).bytes;
-}
-
-extern "C" int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, void* stream) {
-  Paged p{};
-  const int rc = check_paged("ooo_paged_plan", batch, p);
-  if (rc != OOO_OK) return rc;
-  OOO_REQUIRE(plan, OOO_ERR_INVALID, "ooo_paged_plan: null pointer");
-  OOO_REQUIRE(aligned16(plan), OOO_ERR_UNSUPPORTED, "ooo_paged_plan: plan is not 16-byte aligned");
+int make_plan(const char* who, const ooo_paged_batch* batch, const Paged& p, bool eight, void* plan,
+              size_t plan_bytes, void* stream) {
+  OOO_REQUIRE(plan, OOO_ERR_INVALID, "%s: null pointer", who);
+  OOO_REQUIRE(aligned16(plan), OOO_ERR_UNSUPPORTED, "%s: plan is not 16-byte aligned", who);
   const PlanShape s = plan_shape(*batch);
-  OOO_REQUIRE(plan_grid_ok(*batch, s), OOO_ERR_UNSUPPORTED, "ooo_paged_plan: more than 2^30 workgroups");
-  OOO_REQUIRE(plan_bytes >= (size_t)s.bytes, OOO_ERR_CAPACITY, "ooo_paged_plan: plan of %lld bytes needed (got %zu)",
+  OOO_REQUIRE(plan_grid_ok(*batch, s), OOO_ERR_UNSUPPORTED, "%s: more than 2^30 workgroups", who);
+  OOO_REQUIRE(plan_bytes >= (size_t)s.bytes, OOO_ERR_CAPACITY, "%s: plan of %lld bytes needed (got %zu)", who,
               s.bytes, plan_bytes);
   PlanHead head{};
-  plan_key(*batch, head.key);
+  plan_key(*batch, eight, head.key);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  plan_kernel<<<1, kPlanThreads, 0, st>>>(p, s, head, batch->head_dim == 64, (uint8_t*)plan);
+  plan_kernel<<<1, kPlanThreads, 0, st>>>(p, s, eight ? kCosts8 : kCosts, head, batch->head_dim == 64,
+                                          (uint8_t*)plan);
   const long long q = (long long)p.n_rows * p.G;
   plan_rows_kernel<<<(unsigned)((q + 255) / 256), 256, 0, st>>>(p, s, (uint8_t*)plan);
   const hipError_t e = hipGetLastError();
-  OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "ooo_paged_plan: launch failed: %s", hipGetErrorString(e));
+  OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
   return ooo::ok();
 }
 
-extern "C" size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch) {
-  Paged p{};
-  if (check_paged("ooo_paged_attn_workspace", batch, p) != OOO_OK) return 0;
-  return workspace_bytes(*batch, plan_shape(*batch));
-}
-
-extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_bytes, const void* q,
-                              const void* k_pages, const void* v_pages, float scale, void* out, void* workspace,
-                              size_t ws_bytes, void* stream) {
-  PagedAttnArgs a{};
-  const int rc = check_paged("ooo_paged_attn", batch, a.p);
-  if (rc != OOO_OK) return rc;
-  OOO_REQUIRE(plan && q && k_pages && v_pages && out && workspace, OOO_ERR_INVALID, "ooo_paged_attn: null pointer");
+// a: with the batch, and the cache where it is one of 8 bits.
+int attend(const char* who, const ooo_paged_batch* batch, PagedAttnArgs& a, bool eight, const void* plan,
+           size_t plan_bytes, const void* q, const void* k_pages, const void* v_pages, float scale, void* out,
+           void* workspace, size_t ws_bytes, void* stream) {
+  OOO_REQUIRE(plan && q && k_pages && v_pages && out && workspace, OOO_ERR_INVALID, "%s: null pointer", who);
   OOO_REQUIRE(aligned16(plan) && aligned16(q) && aligned16(k_pages) && aligned16(v_pages) && aligned16(out) &&
                   aligned16(workspace),
-              OOO_ERR_UNSUPPORTED, "ooo_paged_attn: a pointer is not 16-byte aligned");
+              OOO_ERR_UNSUPPORTED, "%s: a pointer is not 16-byte aligned", who);
   const float scale_log2e = scale * 1.4426950408889634f;
-  OOO_REQUIRE(fabsf(scale_log2e) < INFINITY, OOO_ERR_INVALID, "ooo_paged_attn: scale %g is not finite in base 2",
+  OOO_REQUIRE(fabsf(scale_log2e) < INFINITY, OOO_ERR_INVALID, "%s: scale %g is not finite in base 2", who,
               (double)scale);
   const PlanShape s = plan_shape(*batch);
-  OOO_REQUIRE(plan_grid_ok(*batch, s), OOO_ERR_UNSUPPORTED, "ooo_paged_attn: more than 2^30 workgroups");
-  OOO_REQUIRE(plan_bytes >= (size_t)s.bytes, OOO_ERR_CAPACITY, "ooo_paged_attn: plan of %lld bytes needed (got %zu)",
+  OOO_REQUIRE(plan_grid_ok(*batch, s), OOO_ERR_UNSUPPORTED, "%s: more than 2^30 workgroups", who);
+  OOO_REQUIRE(plan_bytes >= (size_t)s.bytes, OOO_ERR_CAPACITY, "%s: plan of %lld bytes needed (got %zu)", who,
               s.bytes, plan_bytes);
   const size_t need = workspace_bytes(*batch, s);
-  OOO_REQUIRE(ws_bytes >= need, OOO_ERR_CAPACITY, "ooo_paged_attn: workspace of %zu bytes needed (got %zu)", need,
+  OOO_REQUIRE(ws_bytes >= need, OOO_ERR_CAPACITY, "%s: workspace of %zu bytes needed (got %zu)", who, need,
               ws_bytes);
-  plan_key(*batch, a.want.key);
+  plan_key(*batch, eight, a.want.key);
   a.plan = (const uint8_t*)plan;
   a.off_first_w = s.off_first_w;
   a.off_first_n = s.off_first_n;
@@ -760,11 +781,80 @@ extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, si
     a.scale_log2e = fmaxf(fabsf(scale_log2e), 0x1p-149f);
   }
   const bool neg = scale_log2e < 0.f;
-  if (bf && wide) launch_attn<uint16_t, 128>(a, s, neg, st);
-  else if (bf) launch_attn<uint16_t, 64>(a, s, neg, st);
-  else if (wide) launch_attn<float, 128>(a, s, neg, st);
-  else launch_attn<float, 64>(a, s, neg, st);
+  if (bf && wide) launch_attn<uint16_t, 128>(a, s, eight, neg, st);
+  else if (bf) launch_attn<uint16_t, 64>(a, s, eight, neg, st);
+  else if (wide) launch_attn<float, 128>(a, s, eight, neg, st);
+  else launch_attn<float, 64>(a, s, eight, neg, st);
   const hipError_t e = hipGetLastError();
-  OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "ooo_paged_attn: launch failed: %s", hipGetErrorString(e));
+  OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
   return ooo::ok();
+}
+
+}  // namespace
+}  // namespace ooo
+
+using namespace ooo;
+
+extern "C" size_t ooo_paged_plan_bytes(const ooo_paged_batch* batch) {
+  Paged p{};
+  if (check_paged("ooo_paged_plan_bytes", batch, p) != OOO_OK) return 0;
+  return (size_t)plan_shape(*batch).bytes;
+}
+
+extern "C" int ooo_paged_plan(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, void* stream) {
+  Paged p{};
+  const int rc = check_paged("ooo_paged_plan", batch, p);
+  if (rc != OOO_OK) return rc;
+  return make_plan("ooo_paged_plan", batch, p, false, plan, plan_bytes, stream);
+}
+
+extern "C" size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch) {
+  Paged p{};
+  if (check_paged("ooo_paged_attn_workspace", batch, p) != OOO_OK) return 0;
+  return workspace_bytes(*batch, plan_shape(*batch));
+}
+
+extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_bytes, const void* q,
+                              const void* k_pages, const void* v_pages, float scale, void* out, void* workspace,
+                              size_t ws_bytes, void* stream) {
+  PagedAttnArgs a{};
+  const int rc = check_paged("ooo_paged_attn", batch, a.p);
+  if (rc != OOO_OK) return rc;
+  return attend("ooo_paged_attn", batch, a, false, plan, plan_bytes, q, k_pages, v_pages, scale, out, workspace,
+                ws_bytes, stream);
+}
+
+extern "C" size_t ooo_paged_plan8_bytes(const ooo_paged_batch* batch) {
+  Paged p{};
+  Cache8 c{};
+  if (check_cache8("ooo_paged_plan8_bytes", batch, nullptr, p, c) != OOO_OK) return 0;
+  return (size_t)plan_shape(*batch).bytes;
+}
+
+extern "C" int ooo_paged_plan8(const ooo_paged_batch* batch, void* plan, size_t plan_bytes, void* stream) {
+  Paged p{};
+  Cache8 c{};
+  const int rc = check_cache8("ooo_paged_plan8", batch, nullptr, p, c);
+  if (rc != OOO_OK) return rc;
+  return make_plan("ooo_paged_plan8", batch, p, true, plan, plan_bytes, stream);
+}
+
+extern "C" size_t ooo_paged_attn8_workspace(const ooo_paged_batch* batch) {
+  Paged p{};
+  Cache8 c{};
+  if (check_cache8("ooo_paged_attn8_workspace", batch, nullptr, p, c) != OOO_OK) return 0;
+  return workspace_bytes(*batch, plan_shape(*batch));
+}
+
+extern "C" int ooo_paged_attn8(const ooo_paged_batch* batch, const ooo_cache8* cache, int32_t layer,
+                               const void* plan, size_t plan_bytes, const void* q, float scale, void* out,
+                               void* workspace, size_t ws_bytes, void* stream) {
+  const char* const who = "ooo_paged_attn8";
+  PagedAttnArgs a{};
+  OOO_REQUIRE(cache, OOO_ERR_INVALID, "%s: cache is null", who);
+  int rc = check_cache8(who, batch, cache, a.p, a.c);
+  if (rc == OOO_OK) rc = take_layer(who, cache, layer, a.c);
+  if (rc != OOO_OK) return rc;
+  return attend(who, batch, a, true, plan, plan_bytes, q, a.c.pages[0], a.c.pages[1], scale, out, workspace, ws_bytes,
+                stream);
 }

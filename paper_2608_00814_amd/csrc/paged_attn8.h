@@ -1,0 +1,557 @@
+// Attention with bf16 queries over one item of the plan where the pages hold
+// 8-bit numbers (ooo_paged_attn8), on the matrix cores.
+//
+// The work, its items and the order of operands are those of paged_attn_bf16.h.
+// A tile's rows are copied to LDS as they are, half the bytes, and become bf16
+// on their way into a product: eight numbers of a key (or, for V^T, of a column:
+// ds_read_b64_tr_b8 turns 8 x 16 of them) are eight bytes of a lane, and four
+// v_cvt_scalef32_pk_bf16_fp8, which multiply by the block's power of two for
+// nothing.  Both are exact, so scores and outputs are those of a bf16 cache with
+// the same numbers.  (The 8-bit matrix product, with the queries split into two
+// 8-bit numbers, would save K's conversion, but it adds the 32 products of a
+// step aligned to the largest of them with some 14 bits: 2e-5 of the sum of
+// their sizes is lost where float32 loses 1e-7.)
+#pragma once
+
+#include "attn_tile.h"
+#include "paged_attn_bf16.h"
+
+namespace ooo {
+
+// The LDS DMA of 4 bytes per lane from an address of the lane's own.
+__device__ __forceinline__ void dma4_at(unsigned long long addr, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(addr) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4_nt(const void* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2 nt" ::"s"(lds), "v"(voff), "s"(base)
+               : "memory", "m0");
+}
+
+// LDS geometry of tiles of 8-bit rows: row-major, the 16-byte chunks of a row
+// permuted so that both the K reads (16 rows, one chunk) and the V transpose
+// reads (8 rows, two chunks) lie in distinct banks.
+template <int D>
+struct Ring8 {
+  static constexpr int CH = D / 16;         // chunks of a row
+  static constexpr int MAT = kTile * D;     // bytes of a tile of K or V
+  static constexpr int HALF = 32 * D;       // of a half-tile, the rows of one scale
+  static constexpr int BYTES = 128 * 1024;  // of the ring: 16 KiB a wave
+  static __device__ __forceinline__ int swz(int r, int c) {
+    return c ^ (D == 128 ? (r & 6) | ((r >> 3) & 1) : ((r >> 1) & 2) | ((r >> 3) & 1));
+  }
+};
+
+// Where the half-tiles that one wave copies and reads lie, and their scales.
+// Step n is the 32 keys from k0 + n step on; lane l holds the address of step
+// `base` + l.  Addresses are taken 64 steps at a time (turn), when the scales of
+// those steps are asked for, and the page ids of the next 64; they go through
+// LDS and have landed long before they are read: the waits for the tiles leave
+// only the last requests on their way.
+struct Window8 {
+  static constexpr int BYTES = 6 * 256;  // of LDS a wave: page ids, then scales of K and of V, two of each
+  const int32_t* ids;
+  const uint8_t *ks, *vs;
+  long long stride, head, scale_stride, scale_head;
+  int k0, step, last, count, shift, n_pages, lane, row_bytes;
+  uint8_t* buf;
+  int base, sbase;
+  uint32_t lo, hi, lds, kx, vx;
+  bool bad;
+  __device__ __forceinline__ int key(int n) const { return min(k0 + n * step, last); }
+  __device__ __forceinline__ void start() {
+    lds = __builtin_amdgcn_readfirstlane(lds_addr(buf));
+    base = 0;
+    sbase = -64;
+    kx = vx = 0;
+    bad = false;
+    take(ids[key(lane) >> shift]);
+    ask();
+  }
+  __device__ __forceinline__ uint32_t* word(int x, int n) const {
+    return reinterpret_cast<uint32_t*>(buf + x * 512 + (n & 64) * 4) + lane;
+  }
+  __device__ __forceinline__ void take(int id) {
+    const bool ok = id >= 0 && id < n_pages;
+    bad = bad || __any(!ok);
+    const long long page = ok ? id : 0;
+    const int row = key(base + lane) & ((1 << shift) - 1);
+    const unsigned long long at = (unsigned long long)(page * stride + head + (long long)(row & -32) * row_bytes);
+    lo = (uint32_t)at;
+    hi = (uint32_t)(at >> 32);
+    // the words that the scales lie in
+    const long long off = page * scale_stride + scale_head + row / kBlockRows;
+    const unsigned long long k = (unsigned long long)(uintptr_t)(ks + off), v = (unsigned long long)(uintptr_t)(vs + off);
+    *word(0, base) = (uint32_t)(8 * (k & 3) | 256 * 8 * (v & 3));
+    dma4_at(k & ~3ull, lds + 512 + (base & 64) * 4);
+    dma4_at(v & ~3ull, lds + 1024 + (base & 64) * 4);
+  }
+  __device__ __forceinline__ void ask() const {
+    if (base + 64 >= count) return;
+    dma4(ids, (uint32_t)(key(base + 64 + lane) >> shift) * 4u, lds + ((base + 64) & 64) * 4);
+  }
+  // Before at(n), for rising n.
+  __device__ __forceinline__ void turn(int n) {
+    if (n - base < 64) return;
+    base += 64;
+    take((int)*word(0, base));
+    ask();
+  }
+  __device__ __forceinline__ long long at(int n) const {
+    return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readlane(hi, n - base) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane(lo, n - base));
+  }
+  // Before scale(n), for rising n, behind the wait for step n's keys.
+  __device__ __forceinline__ void turn_scales(int n) {
+    if (n - sbase < 64) return;
+    sbase += 64;
+    const uint32_t sh = *word(0, sbase);
+    kx = (*word(1, sbase) >> (sh & 31) & 255) << 23;
+    vx = (*word(2, sbase) >> (sh >> 8 & 31) & 255) << 23;
+  }
+  __device__ __forceinline__ float k_scale(int n) const {
+    return __uint_as_float(__builtin_amdgcn_readlane(kx, n - sbase));
+  }
+  __device__ __forceinline__ float v_scale(int n) const {
+    return __uint_as_float(__builtin_amdgcn_readlane(vx, n - sbase));
+  }
+};
+
+// Eight numbers times a power of two.
+__device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float up) {
+  return as_bf16x8(u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, up, false)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, up, true)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, up, false)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, up, true))});
+}
+
+// One item by a workgroup (WIDE; every wave calls it) or by a wave alone.
+template <int D, bool NEG, bool WIDE>
+__device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int wave, uint8_t* ring,
+                                                 uint64_t* mwords, uint8_t* windows, int* bad_s) {
+  using R = Ring8<D>;
+  constexpr int NW = kPagedWaves, RG = 4, NP = D / 8, DT = D / 32, S = D / 16;
+  constexpr int V0 = 4 * R::MAT;       // of a wide ring: four stages of K, then of V
+  constexpr int HI = R::HALF / 1024;   // DMA instructions of a half-tile
+  constexpr int NS = 16384 / (2 * R::HALF);  // stages of a narrow wave
+  constexpr int kJoinMl = RG * NP * 64 * 16;  // where the joined halves' statistics lie, behind their sums
+  static_assert(8 * R::MAT <= R::BYTES && kJoinMl + RG * 64 * 8 <= R::BYTES, "ring");
+  const PagedAttnArgs& a = args_again();
+  const Paged p = a.p;
+  const float scale = a.scale_log2e;
+  const Item it = load_item(a.plan + (WIDE ? a.off_items_w : a.off_items_n), item);
+  const int rg = WIDE ? wave % RG : 0, kh0 = WIDE ? wave / RG : 0;
+  const int c = lane & 31, u = lane >> 5;
+  const int qr = rg * 32 + c;                    // row of the block
+  const bool on = qr < it.nq;
+  const bool idle = rg * 32 >= it.nq;            // the whole group is past the block's rows
+  const int qi = it.q0 + min(qr, it.nq - 1), i = qi / p.G, hq = g * p.G + qi - i * p.G;
+  const long long row = (long long)it.row0 + i;
+  // The queries: products 2 j and 2 j + 1 of a score take a key's 16 columns
+  // 16 (2 j + u) on, as one read of K gives them.
+  bf16x8 qf[S];
+  {
+    const uint16_t* qrow = (const uint16_t*)a.q + (row * p.Hq + hq) * D;
+#pragma unroll
+    for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(ld16(qrow + 16 * (2 * (x / 2) + u) + 8 * (x & 1)));
+  }
+  Window8 window;
+  window.ids = it.flags & kShared ? p.shared_pages : p.table + (size_t)it.seq * p.table_ld;
+  window.ks = a.c.scales[0];
+  window.vs = a.c.scales[1];
+  window.stride = p.page_stride;
+  window.head = ((long long)g << p.page_shift) * D;
+  window.scale_stride = a.c.scale_stride;
+  window.scale_head = (long long)g * a.c.page_blocks;
+  window.k0 = WIDE ? kTileKeys * it.t0 + 32 * kh0 : 32 * it.t0;
+  window.step = WIDE ? kTileKeys : 32;
+  window.last = it.limit - 1;
+  window.count = it.t1 - it.t0;
+  window.shift = p.page_shift;
+  window.n_pages = p.n_pages;
+  window.lane = lane;
+  window.row_bytes = D;
+  window.buf = windows + wave * Window8::BYTES;
+  window.start();
+  const int all = all_see(p, it);
+  const uint8_t* const kp = (const uint8_t*)a.k;
+  const uint8_t* const vp = (const uint8_t*)a.v;
+
+  // LDS addresses of the fragments in the wave's first stage.  K read j: chunk
+  // 2 j + u of row sigma(c), 32 j bytes away by the permutation's exclusive or.
+  // V transpose read (16 keys kk, column block dt): row 16 kk + 8 (g16 / 2) +
+  // li / 2, chunk 2 dt + g16 % 2, its half li % 2: 32 dt bytes away.
+  const uint32_t k_lds = lds_addr(ring) + (WIDE ? kh0 * R::HALF : wave * 16384);
+  const uint32_t v_lds = k_lds + (WIDE ? V0 : R::HALF);
+  const int krow = sigma(c), g16 = lane >> 4, li = lane & 15;
+  const int vrow = 8 * (g16 >> 1) + (li >> 1);
+  uint32_t k_at = k_lds + krow * D + (R::swz(krow, u) << 4);
+  uint32_t v_at = v_lds + vrow * D + (R::swz(vrow, g16 & 1) << 4) + 8 * (li & 1);
+
+  // Ends the wait for the queries here: inside the loops it would be a wait for
+  // the DMA in flight.  A negative scale (NEG) turns their signs, which is exact,
+  // so that the largest score is the largest product and unseen keys stay at
+  // -inf.
+  auto queries_here = [&]() OOO_INLINE {
+#pragma unroll
+    for (int x = 0; x < S; ++x) asm volatile("" : "+v"(qf[x]));
+    if constexpr (NEG) {
+#pragma unroll
+      for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(__builtin_bit_cast(u32x4, qf[x]) ^ 0x80008000u);
+    }
+  };
+  f32x16 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // ---- arithmetic of one half-tile (32 keys)
+  auto kread1 = [&](int j) OOO_INLINE {
+    return *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)(k_at ^ (32u * j));
+  };
+  auto kread = [&](u32x4 (&kr)[DT]) OOO_INLINE {
+#pragma unroll
+    for (int j = 0; j < DT; ++j) kr[j] = kread1(j);
+  };
+  auto score1 = [&](int x, const u32x4 (&kr)[DT], float up, const f32x16& acc) OOO_INLINE {
+    return mfma32(bf16_of(kr[x / 2][2 * (x & 1)], kr[x / 2][2 * (x & 1) + 1], up), qf[x], acc);
+  };
+  auto scores = [&](const u32x4 (&kr)[DT], float up) OOO_INLINE {
+    f32x16 acc = f32x16{};
+#pragma unroll
+    for (int x = 0; x < S; ++x) acc = score1(x, kr, up, acc);
+    return acc;
+  };
+  auto vread = [&](int x) OOO_INLINE {  // 16 keys x / DT, column block x % DT
+    return __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                   (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32u * (x % DT))) + 16 * (x / DT) * D)));
+  };
+  auto pv = [&](int x, const u32x2& v, float up, const bf16x8 (&pr)[2]) OOO_INLINE {
+    oacc[x % DT] = mfma32(bf16_of(v[0], v[1], up), pr[x / DT], oacc[x % DT]);
+  };
+  auto row_max = [&](const f32x16& s, auto between) OOO_INLINE {
+    float m0 = max3f(s[0], s[1], s[2]), m1 = max3f(s[8], s[9], s[10]);
+    m0 = max3f(m0, s[3], s[4]);
+    m1 = max3f(m1, s[11], s[12]);
+    between();
+    m0 = max3f(m0, s[5], s[6]);
+    m1 = max3f(m1, s[13], s[14]);
+    const float mx = max3f(max3f(m0, s[7], m1), s[15], -INFINITY);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    return max3f(__uint_as_float(sw[0]), __uint_as_float(sw[1]), -INFINITY) * scale;
+  };
+  auto masked = [&](f32x16& s, int lo, const uint64_t* words) OOO_INLINE {
+    if (lo + 32 > all) {
+      // lane value j is key 16 (j / 8) + 8 u + j % 8
+      const uint32_t b = (uint32_t)seen_in(p, it, i, words, lo) >> (8 * u);
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (!((b >> (16 * (j / 8) + j % 8)) & 1u)) s[j] = -INFINITY;
+    }
+  };
+  // The reference maximum moves only when some row grows by more than 2^8, so
+  // probabilities stay <= 256 and O, l are rescaled rarely.
+  auto new_max = [&](float mx) OOO_INLINE {
+    if (__any(mx > m_run + 8.f)) {
+      const float m_new = __builtin_fmaxf(m_run, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) oacc[dt] *= alpha;
+      m_run = m_new;
+    }
+    return m_run == -INFINITY ? 0.f : m_run;
+  };
+  // Probabilities, two at a time, each pair behind the next pair's exponents;
+  // between(k) goes with pair k.  They go into the product rounded to bf16, the
+  // matrix cores' operand, and the rounded ones into the sum: the weights that
+  // multiply V then sum to one, and the rounding (half a step, 2^-8, each)
+  // moves an output by that share of sum p |v - out| alone.
+  auto weights = [&](const f32x16& s, float m_use, bf16x8 (&pf)[2], auto between) OOO_INLINE {
+    float x[2] = {fmaf(s[0], scale, -m_use), fmaf(s[1], scale, -m_use)};
+    float pr[2][2], ps[2] = {0.f, 0.f};
+    u32x4 pk[2];
+#pragma unroll
+    for (int k = 0; k <= 8; ++k) {
+      if (k < 8) between(k);
+      if (k < 8) {
+        pr[k & 1][0] = __builtin_amdgcn_exp2f(x[0]);
+        pr[k & 1][1] = __builtin_amdgcn_exp2f(x[1]);
+        asm volatile("" : "+v"(pr[k & 1][0]), "+v"(pr[k & 1][1]));  // not later
+      }
+      if (k < 7) {
+        x[0] = fmaf(s[2 * k + 2], scale, -m_use);
+        x[1] = fmaf(s[2 * k + 3], scale, -m_use);
+      }
+      if (k > 0) {
+        const float* e = pr[(k - 1) & 1];
+        pk[(k - 1) / 4][(k - 1) % 4] = pack_bf16x2(e[0], e[1]);
+        ps[k & 1] = add_bf16x2(pk[(k - 1) / 4][(k - 1) % 4], ps[k & 1]);
+      }
+    }
+    pf[0] = as_bf16x8(pk[0]);
+    pf[1] = as_bf16x8(pk[1]);
+    l_run += ps[0] + ps[1];
+  };
+
+  if constexpr (WIDE) {
+    if (threadIdx.x == 0) *bad_s = 0;
+    const int tiles = it.t1 - it.t0;
+    // mask words of the block's rows, for the tiles that hold new rows
+    if (p.W && !(it.flags & kShared) && kTileKeys * it.t1 > it.len) {
+      const int n = RG * 32 * 2 * p.W / 64;
+      for (int j = wave; j < n; j += NW) {
+        const int e = j * 64 + lane, r = e / (2 * p.W), k = e - r * (2 * p.W);
+        const int node = (it.q0 + min(r, it.nq - 1)) / p.G;
+        dma4(p.mask, (uint32_t)((it.row0 + node) * 2 * p.W + k) * 4u, lds_addr(mwords) + j * 256);
+      }
+    }
+    const uint64_t* const words = mwords + qr * p.W;
+    // A wave copies rows 8 wave .. 8 wave + 7 of every tile, which lie in its own
+    // half: 1 KiB at head_dim 128 (16 bytes a lane), 512 bytes at 64 (4 bytes, twice).
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(ring) + wave * 8 * D);
+    auto copy = [&](const uint8_t* pool, int n, uint32_t to) OOO_INLINE {
+      const uint8_t* const src = pool + window.at(n);
+      const int end = it.limit - kTileKeys * (it.t0 + n) - 1;  // rows past the last one repeat it
+      if constexpr (D == 128) {
+        const int r = 8 * wave + lane / 8;
+        dma16_nt(src, (uint32_t)(min(r, end) & 31) * D + (uint32_t)R::swz(r, lane % 8) * 16u, to);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int r = 8 * wave + 4 * x + lane / 16;
+          dma4_nt(src, (uint32_t)(min(r, end) & 31) * D + (uint32_t)R::swz(r, lane % 16 / 4) * 16u + lane % 4 * 4u,
+                  to + x * 256);
+        }
+      }
+    };
+    queries_here();
+    for (int n = 0; n < tiles; ++n) {
+      window.turn(n);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      wg_barrier();  // nobody reads the tile before
+      copy(kp, n, dst);
+      copy(vp, n, dst + V0);
+      wait_vmcnt<0>();
+      wg_barrier();
+      if (idle) continue;
+      window.turn_scales(n);
+      u32x4 kr[DT];
+      u32x2 vv[S];
+      bf16x8 pf[2];
+      kread(kr);
+      f32x16 sc = scores(kr, window.k_scale(n));
+      masked(sc, kTileKeys * (it.t0 + n) + 32 * kh0, words);
+      settle(sc);
+      weights(sc, new_max(row_max(sc, []() {})), pf, [](int) {});
+#pragma unroll
+      for (int x = 0; x < S; ++x) vv[x] = vread(x);
+      const float up = window.v_scale(n);
+#pragma unroll
+      for (int x = 0; x < S; ++x) pv(x, vv[x], up, pf);
+    }
+  } else {
+    const uint32_t kd = __builtin_amdgcn_readfirstlane(k_lds), vd = kd + R::HALF;
+    uint32_t full_off[HI];
+    const int rpi = 1024 / D;
+#pragma unroll
+    for (int x = 0; x < HI; ++x) {
+      const int r = x * rpi + lane / R::CH;
+      full_off[x] = (uint32_t)r * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
+    }
+    auto ask = [&](const uint8_t* pool, int n, uint32_t dst) OOO_INLINE {
+      const uint8_t* const src = pool + window.at(n);
+      const int end = it.limit - 32 * (it.t0 + n) - 1;
+#pragma unroll
+      for (int x = 0; x < HI; ++x) {
+        uint32_t off = full_off[x];
+        if (end < 31) {
+          const int r = x * rpi + lane / R::CH;
+          off = (uint32_t)min(r, end) * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
+        }
+        dma16_nt(src, off, dst + x * 1024);
+      }
+    };
+    const uint64_t* const words = p.mask + (size_t)row * p.W;
+    const int count = it.t1 - it.t0;
+    queries_here();
+    for (int n = 0; n < count; ++n) {
+      window.turn(n);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      ask(kp, n, kd);
+      ask(vp, n, vd);
+      wait_vmcnt<0>();
+      window.turn_scales(n);
+      u32x4 kr[DT];
+      u32x2 vv[S];
+      bf16x8 pf[2];
+      kread(kr);
+      f32x16 sc = scores(kr, window.k_scale(n));
+      masked(sc, 32 * (it.t0 + n), words);
+      settle(sc);
+      weights(sc, new_max(row_max(sc, []() {})), pf, [](int) {});
+#pragma unroll
+      for (int x = 0; x < S; ++x) vv[x] = vread(x);
+      const float up = window.v_scale(n);
+#pragma unroll
+      for (int x = 0; x < S; ++x) pv(x, vv[x], up, pf);
+    }
+  }
+  bool bad = window.bad;
+
+  const PagedAttnArgs& ea = args_again();
+  const Paged& ep = ea.p;
+  const Item e = load_item(ea.plan + (WIDE ? ea.off_items_w : ea.off_items_n), item);
+  const int eq = e.q0 + min(qr, e.nq - 1), ei = eq / ep.G;
+  const long long row_e = (long long)e.row0 + ei;
+
+  // A value of V that is not finite counts only for the rows that give its key
+  // a weight, but the products multiply it by the zeros of the others, and
+  // zero times it is NaN.  So a wave with a row of such sums adds its keys once
+  // more, one by one, without those of weight zero.  A row whose weights are not
+  // finite (its query, or a key that it sees) is NaN either way and no reason
+  // to: 64 rows over a 4k prompt took 1600 us, not 41, for one NaN query.
+  if (!idle) {
+    float z = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) z = __builtin_fmaf(oacc[dt][j], 0.f, z);
+    bool again = __any(!(z == 0.f));
+    if (again) again = __any(!(z == 0.f) && l_run + shfl_xor_f(l_run, 32) < INFINITY);
+    if (again) {
+      const Pages pages(ep, e);
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      l_run = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = f32x16{};
+      const int step = WIDE ? 2 : 1, h1 = WIDE ? 2 * e.t1 : e.t1;
+      for (int h = WIDE ? 2 * e.t0 + kh0 : e.t0; h < h1 && 32 * h < e.limit; h += step) {
+        const uint64_t bits = seen(ep, e, ei, (int)row_e, 32 * h);
+#pragma unroll 1
+        for (int j = 0; j < 32 && 32 * h + j < e.limit; ++j) {
+          const int t = 32 * h + j;
+          const int page = pages.at(t, bad), pr = t & ((1 << ep.page_shift) - 1);
+          const long long base = (long long)page * ep.page_stride + (((long long)g << ep.page_shift) + pr) * D;
+          const long long so = (long long)page * ea.c.scale_stride + (long long)g * ea.c.page_blocks + pr / kBlockRows;
+          const float ku = scale_of(ea.c.scales[0] + so), vu = scale_of(ea.c.scales[1] + so);
+          float s = 0.f;
+#pragma unroll
+          for (int y = 0; y < DT; ++y) {
+            const u32x4 kk = ld16((const uint8_t*)ea.k + base + 16 * (2 * y + u));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const bf16x8 kb = bf16_of(kk[2 * h], kk[2 * h + 1], ku);
+#pragma unroll
+              for (int x = 0; x < 8; ++x) s = __builtin_fmaf((float)kb[x], (float)qf[2 * y + h][x], s);
+            }
+          }
+          s += shfl_xor_f(s, 32);
+          const float w = (bits >> j) & 1 ? __builtin_amdgcn_exp2f(fmaf(s, ea.scale_log2e, -m_use)) : 0.f;
+          if (w == 0.f) continue;
+          if (u == 0) l_run += w;
+#pragma unroll
+          for (int q = 0; q < NP; ++q) {
+            float x[4];
+            values4(*reinterpret_cast<const uint32_t*>((const uint8_t*)ea.v + base + 8 * q + 4 * u), vu, x);
+            f32x16& o = oacc[q / 4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) o[4 * (q % 4) + y] += w * x[y];
+          }
+        }
+      }
+    }
+  }
+
+  float l_tot = l_run + shfl_xor_f(l_run, 32);
+  if constexpr (WIDE) {
+    if (__any(bad)) *bad_s = 1;
+    wait_vmcnt<0>();
+    __syncthreads();  // the ring is free, bad_s complete
+  }
+  auto piece = [&](int q) OOO_INLINE {
+    return f32x4{oacc[q / 4][4 * (q % 4)], oacc[q / 4][4 * (q % 4) + 1], oacc[q / 4][4 * (q % 4) + 2],
+                 oacc[q / 4][4 * (q % 4) + 3]};
+  };
+  uint16_t* const orow = (uint16_t*)ea.out + (row_e * ep.Hq + g * ep.G + eq - ei * ep.G) * D + 4 * u;
+  auto put = [&](int q, f32x4 o, float inv) OOO_INLINE {
+    u32x2 pk;
+    pk[0] = pack_bf16x2(o[0] * inv, o[1] * inv);
+    pk[1] = pack_bf16x2(o[2] * inv, o[3] * inv);
+    *reinterpret_cast<u32x2*>(orow + 8 * q) = pk;
+  };
+  const bool direct = e.flags & kDirect;
+  const size_t sl = (size_t)(e.slot + rg) * ep.Hkv + g;
+  f32x4* const po = reinterpret_cast<f32x4*>(ea.part_o) + sl * NP * 64 + lane;
+  f32x2_t* const pml = reinterpret_cast<f32x2_t*>(ea.part_ml) + sl * 32 + c;
+  if (!direct && e.slot + (e.nq + 31) / 32 > ea.max_slots) return;
+  if constexpr (WIDE) {
+    // join the two key halves of each row group through the ring
+    if (kh0 == 1 && !idle) {
+#pragma unroll
+      for (int q = 0; q < NP; ++q)
+        *reinterpret_cast<f32x4*>(ring + ((rg * NP + q) * 64 + lane) * 16) = piece(q);
+      *reinterpret_cast<f32x2_t*>(ring + kJoinMl + (rg * 64 + lane) * 8) = f32x2_t{m_run, l_tot};
+    }
+    __syncthreads();
+    if (kh0 == 1 || idle) return;
+    const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(ring + kJoinMl + (rg * 64 + lane) * 8);
+    const float mn = __builtin_fmaxf(m_run, ml[0]), base = mn == -INFINITY ? 0.f : mn;
+    const float a0 = __builtin_amdgcn_exp2f(m_run - base), a1 = __builtin_amdgcn_exp2f(ml[0] - base);
+    l_tot = l_tot * a0 + ml[1] * a1;
+    if (*bad_s) l_tot = __builtin_nanf("");
+    const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // a row that sees no key is zero
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      const f32x4 o1 = *reinterpret_cast<const f32x4*>(ring + ((rg * NP + q) * 64 + lane) * 16);
+      f32x4 o = piece(q) * a0;
+      if (a1 > 0.f) o += o1 * a1;
+      if (direct) {
+        if (on) put(q, o, inv);
+      } else {
+        po[q * 64] = o;
+      }
+    }
+    if (!direct && u == 0) *pml = f32x2_t{mn, l_tot};
+  } else if (on) {
+    if (bad) l_tot = __builtin_nanf("");
+    const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      if (direct) put(q, piece(q), inv);
+      else po[q * 64] = piece(q);
+    }
+    if (!direct && u == 0) *pml = f32x2_t{m_run, l_tot};
+  }
+}
+
+template <int D, bool NEG>
+__global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttnArgs) {
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[Ring8<D>::BYTES];
+  __shared__ __attribute__((aligned(1024))) uint64_t mwords[4 * 32 * 16];
+  __shared__ __attribute__((aligned(1024))) uint8_t windows[kPagedWaves * Window8::BYTES];
+  __shared__ int bad_s;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int g, worker;
+  {
+    const PagedAttnArgs& a = args_again();
+    g = blockIdx.x % a.p.Hkv, worker = blockIdx.x / a.p.Hkv;
+    const PlanHead head = load_head(a);
+    if (!plan_fits(head, a.want)) return;
+    each_wide(a, head, worker, [&](int item) OOO_INLINE {
+      paged_attn8_item<D, NEG, true>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+    });
+  }
+  const PagedAttnArgs& a = args_again();
+  const PlanHead head = load_head(a);
+  const int narrow = worker - head.narrow_first;
+  if (narrow < 0 || narrow >= head.narrow_workers) return;
+  if (head.narrow_first == 0) __syncthreads();  // it may have done wide items
+  const ScalarPtr fn = scalar_ptr(a.plan + a.off_first_n) + narrow * kPagedWaves + wave;
+  const int n0 = fn[0], n1 = min(fn[1], a.max_items_n);
+  for (int item = n0; item < n1; ++item)
+    paged_attn8_item<D, NEG, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+}
+
+}  // namespace ooo

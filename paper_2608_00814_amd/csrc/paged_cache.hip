@@ -5,38 +5,10 @@
 //  * ooo_paged_compact  the accepted rows of every sequence moved together
 #include "paged.h"
 #include "rope.h"
+#include "vec16.h"
 
 namespace ooo {
 namespace {
-
-// 16 bytes as floats and back (round to nearest even).
-template <class T>
-struct Vec16;
-template <>
-struct Vec16<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void unpack(u32x4 v, float (&f)[4]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
-  }
-  static __device__ __forceinline__ u32x4 pack(const float (&f)[4]) {
-    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
-  }
-};
-template <>
-struct Vec16<uint16_t> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void unpack(u32x4 v, float (&f)[8]) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = __uint_as_float(v[e] << 16);
-      f[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
-    }
-  }
-  static __device__ __forceinline__ u32x4 pack(const float (&f)[8]) {
-    return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-  }
-};
 
 // ------------------------------------------------------------------ append
 // x <- x / sqrt(mean(x^2) + eps) w per head, then the rotate-half pairs

@@ -24,7 +24,7 @@
 //  * the last take the narrow blocks' half-tiles of 32 keys in the same way, a
 //    run for each of their waves.
 // The numbers of workgroups and runs are those that finish first by the costs
-// in paged_attn.hip.  The part of a block in one run leaves unnormalised sums and softmax
+// of their kernels (PlanCosts).  The part of a block in one run leaves unnormalised sums and softmax
 // statistics in *slots* of `group` query rows, and a second kernel joins the
 // slots of every row.  A block of one item and without a shared part writes
 // its output itself.
@@ -55,6 +55,15 @@ struct PlanShape {
   int workers;              // workgroups of a KV head
   long long max_blocks, max_items_w, max_items_n, max_slots;
   long long off_blocks, off_seqs, off_first_w, off_first_n, off_items_w, off_items_n, off_rows, bytes;
+};
+
+// Costs in 100 cycles at head_dim 128 (half of them at 64), as measured: a wide
+// tile of a worker; an item's start (its record, pages, queries and first
+// tiles, one behind the other) and end; a half-tile of a narrow worker, whose
+// eight waves have 128 KiB on their way; and a half-tile at the chip's share of
+// the HBM rate.
+struct PlanCosts {
+  float tile, item, half, half_hbm;
 };
 
 // Item record (16 ints).
@@ -132,8 +141,8 @@ inline bool plan_grid_ok(const ooo_paged_batch& b, const PlanShape& s) {
   return (double)s.workers * b.n_kv_heads <= 1073741824.0 && join <= 1073741824.0;
 }
 
-// The sizes that a plan belongs to.
-inline void plan_key(const ooo_paged_batch& b, int (&k)[8]) {
+// The sizes that a plan belongs to (eight: and pages of 8-bit numbers).
+inline void plan_key(const ooo_paged_batch& b, bool eight, int (&k)[8]) {
   k[0] = b.n_seqs;
   k[1] = b.n_rows;
   k[2] = b.n_q_heads;
@@ -141,7 +150,7 @@ inline void plan_key(const ooo_paged_batch& b, int (&k)[8]) {
   k[4] = b.table_ld;
   k[5] = b.shared_len;
   k[6] = b.mask_words;
-  k[7] = (b.page_rows << 12) + b.head_dim * 4 + (int)b.dt + 1;
+  k[7] = (b.page_rows << 12) + b.head_dim * 4 + (int)b.dt + 1 + (eight ? 2 : 0);
 }
 
 }  // namespace ooo

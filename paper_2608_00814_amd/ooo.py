@@ -1,4 +1,4 @@
-"""ctypes binding of libooo (C ABI declared in include/ooo.h and ooo_batch.h).
+"""ctypes binding of libooo (C ABI declared in include/ooo.h, ooo_batch.h and ooo_cache8.h).
 
 Argument marshalling only: every computation happens in the native library.
 Device arguments are torch tensors on the ROCm device (their ``data_ptr()``
@@ -95,6 +95,27 @@ BATCH_SIGNATURES = {
 }
 
 
+class Cache8Struct(ctypes.Structure):
+    """ooo_cache8 of include/ooo_cache8.h."""
+
+    _fields_ = [("k_pages", _vp), ("v_pages", _vp), ("k_scales", _vp), ("v_scales", _vp), ("layer_stride", _i64),
+                ("scale_stride", _i64), ("scale_layer_stride", _i64), ("n_layers", _i32)]
+
+
+# name -> (restype, argtypes); mirrors include/ooo_cache8.h
+CACHE8_SIGNATURES = {
+    "ooo_paged_append8": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _vp, ctypes.c_float, _vp, ctypes.c_double,
+                                         _vp, _vp]),
+    "ooo_paged_plan8_bytes": (_sz, [_vp]),
+    "ooo_paged_plan8": (ctypes.c_int, [_vp, _vp, _sz, _vp]),
+    "ooo_paged_attn8_workspace": (_sz, [_vp]),
+    "ooo_paged_attn8": (ctypes.c_int, [_vp, _vp, _i32, _vp, _sz, _vp, ctypes.c_float, _vp, _vp, _sz, _vp]),
+    "ooo_paged_compact8": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i32, _vp]),
+    "ooo_paged_fork": (ctypes.c_int, [_vp, _vp, _vp, _i32, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "ooo_paged_fork8": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+}
+
+
 class OooError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"[{status}] {message}")
@@ -110,7 +131,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise OSError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_00814_amd.build`")
         h = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in (*SIGNATURES.items(), *BATCH_SIGNATURES.items()):
+        for name, (res, args) in (*SIGNATURES.items(), *BATCH_SIGNATURES.items(), *CACHE8_SIGNATURES.items()):
             f = getattr(h, name)
             f.restype = res
             f.argtypes = args
@@ -558,10 +579,13 @@ class PagedBatch:
     int32; k_pages [n_pages][Hkv][page_rows][D], one layer's pool (v_pages has
     its shape and strides; pages may lie apart, as where the pools of several
     layers are interleaved); n_rows rows of q, qkv and out; shared_pages int32
-    with shared_len tokens, or None; anc_mask [>= n_rows][words] int64, or None."""
+    with shared_len tokens, or None; anc_mask [>= n_rows][words] int64, or None.
+
+    A pool of float8_e4m3fn is one layer's of an 8-bit cache (``Cache8``); dtype
+    is then the type of q, qkv, the norms and out, bfloat16 or float32."""
 
     def __init__(self, row_start, seq_len, page_table, k_pages, n_q_heads: int, n_rows: int, shared_pages=None,
-                 shared_len: int = 0, anc_mask=None):
+                 shared_len: int = 0, anc_mask=None, dtype=None):
         import torch
 
         dev = k_pages.device
@@ -587,8 +611,14 @@ class PagedBatch:
             b.mask_words = anc_mask.shape[1]
         b.n_seqs, b.n_rows, b.table_ld, b.shared_len = n, n_rows, page_table.shape[1], shared_len
         b.page_rows, b.n_pages, b.n_q_heads, b.n_kv_heads, b.head_dim = rows, n_pages, n_q_heads, Hkv, D
-        b.dt = dtype_code(k_pages)
-        self.device, self.dtype, self.pool = dev, k_pages.dtype, tuple(k_pages.shape)
+        self.pool_dtype, self.eight = k_pages.dtype, k_pages.dtype == torch.float8_e4m3fn
+        self.dtype = k_pages.dtype if dtype is None and not self.eight else dtype
+        if not self.eight and self.dtype != k_pages.dtype:
+            raise ValueError(f"dtype must be that of k_pages, {k_pages.dtype}, not {dtype}")
+        if self.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"dtype must be torch.float32 or torch.bfloat16, not {self.dtype}")
+        b.dt = F32 if self.dtype == torch.float32 else BF16
+        self.device, self.pool = dev, tuple(k_pages.shape)
         self.n_seqs, self.n_rows, self.Hq, self.Hkv, self.D = n, n_rows, n_q_heads, Hkv, D
         b.page_stride = self.page_stride = self._stride_of(k_pages, "k_pages")
         self._keep = (row_start, seq_len, page_table, shared_pages, anc_mask)
@@ -605,10 +635,12 @@ class PagedBatch:
             raise ValueError(f"{name}: pages overlap")
         return s
 
-    def pool_ptr(self, t, name: str) -> int:
-        """Address of a pool of this batch, after its checks."""
-        if t.device != self.device or t.dtype != self.dtype:
-            raise ValueError(f"{name} must be {self.dtype} on {self.device}")
+    def pool_ptr(self, t, name: str, eight: bool = False) -> int:
+        """Address of a pool of this batch, after its checks (eight: of an 8-bit cache)."""
+        if self.eight != eight:
+            raise ValueError(f"the batch's pages hold {self.pool_dtype}: not for this call")
+        if t.device != self.device or t.dtype != self.pool_dtype:
+            raise ValueError(f"{name} must be {self.pool_dtype} on {self.device}")
         if self._stride_of(t, name) != self.page_stride:
             raise ValueError(f"{name}: pages lie {t.stride(-4)} elements apart, the batch's {self.page_stride}")
         return t.data_ptr()
@@ -702,6 +734,169 @@ def paged_compact(batch: PagedBatch, k_pages, v_pages, path, accept_len, stream=
                                    _on(path, "path", batch.device, torch.int32, (batch.n_seqs, cap)),
                                    _on(accept_len, "accept_len", batch.device, torch.int32, (batch.n_seqs,)), cap,
                                    _stream_on(batch.device, stream)))
+
+
+# ----------------------------------------------------------------------------
+# 8-bit cache pages, and sequences that continue others
+
+BLOCK_ROWS = 32  # rows of a page that share a scale
+
+
+class Cache8:
+    """ooo_cache8 over torch tensors, which it keeps alive: for a batch whose
+    pool is of float8_e4m3fn, k_pages and v_pages [L][n_pages][Hkv][page_rows][D]
+    (or one layer's), k_scales and v_scales [L][n_pages][Hkv][page_rows / 32] of
+    float8_e8m0fnu or uint8, all with contiguous pages; pages and layers may lie
+    apart."""
+
+    def __init__(self, batch: PagedBatch, k_pages, v_pages, k_scales, v_scales):
+        import torch
+
+        if not batch.eight:
+            raise ValueError(f"the batch's pages hold {batch.pool_dtype}, not float8_e4m3fn")
+        n_pages, Hkv, rows, _ = batch.pool
+        if rows % BLOCK_ROWS:
+            raise ValueError(f"pages of {rows} rows: an 8-bit cache has blocks of {BLOCK_ROWS}")
+        if k_pages.dim() not in (4, 5) or k_pages.dim() != v_pages.dim() or k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages must be [L][n_pages][n_kv_heads][page_rows][head_dim]")
+        many = k_pages.dim() == 5
+        L = k_pages.shape[0] if many else 1
+        if L < 1:
+            raise ValueError("the cache has no layers")
+        c = Cache8Struct()
+        c.k_pages, c.v_pages = batch.pool_ptr(k_pages, "k_pages", True), batch.pool_ptr(v_pages, "v_pages", True)
+        c.n_layers, c.layer_stride = L, k_pages.stride(0) if L > 1 else 0
+        page = Hkv * (rows // BLOCK_ROWS)
+        shape = (*k_pages.shape[:-4], n_pages, Hkv, rows // BLOCK_ROWS)
+        strides = []
+        for t, nm in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+            if t.device != batch.device or t.dtype not in (torch.float8_e8m0fnu, torch.uint8):
+                raise ValueError(f"{nm} must be float8_e8m0fnu or uint8 on {batch.device}")
+            if tuple(t.shape) != shape or not t[(0,) * (t.dim() - 2)].is_contiguous():
+                raise ValueError(f"{nm} must be {list(shape)} with contiguous pages")
+            s = t.stride(-3) if n_pages > 1 else max(t.stride(-3), page)
+            if s < page:
+                raise ValueError(f"{nm}: pages overlap")
+            strides.append((s, t.stride(0) if L > 1 else 0))
+        if strides[0] != strides[1] or (L > 1 and k_pages.stride(0) != v_pages.stride(0)):
+            raise ValueError("the pools of K and V must have the same strides")
+        c.scale_stride, c.scale_layer_stride = strides[0]
+        c.k_scales, c.v_scales = k_scales.data_ptr(), v_scales.data_ptr()
+        self._keep = (k_pages, v_pages, k_scales, v_scales)
+        self.n_layers, self.batch_pool, self.page_stride, self.device = L, batch.pool, batch.page_stride, batch.device
+        self.struct = c
+        self.address = ctypes.addressof(c)
+
+    def of(self, batch: PagedBatch) -> int:
+        """The struct's address, for a call with this batch."""
+        if not batch.eight or batch.pool != self.batch_pool or batch.page_stride != self.page_stride:
+            raise ValueError("the cache was made for a batch with other pages")
+        if batch.device != self.device:
+            raise ValueError(f"the cache is on {self.device}, the batch on {batch.device}")
+        return self.address
+
+
+def paged_append8(batch: PagedBatch, cache: Cache8, qkv, q_norm, k_norm, eps: float, rope_theta: float, q_out,
+                  depth=None, layer: int = 0, stream=None) -> None:
+    """As ``paged_append``, into one layer of an 8-bit cache."""
+    import torch
+
+    n, width = batch.n_rows, (batch.Hq + 2 * batch.Hkv) * batch.D
+    if qkv.device != batch.device or qkv.dtype != batch.dtype or tuple(qkv.shape) != (n, width) or qkv.stride(1) != 1:
+        raise ValueError(f"qkv must be [{n}][{width}] {batch.dtype} on {batch.device}")
+    norms = [None if t is None else _on(t, nm, batch.device, batch.dtype, (batch.D,))
+             for t, nm in ((q_norm, "q_norm"), (k_norm, "k_norm"))]
+    dp = None if depth is None else _on(depth, "depth", batch.device, torch.int32, (n,))
+    ld = qkv.stride(0) if n > 1 else max(qkv.stride(0), width)
+    _check(lib().ooo_paged_append8(batch.address, cache.of(batch), layer, qkv.data_ptr(), ld, norms[0], norms[1], eps,
+                                   dp, rope_theta, batch.row_ptr(q_out, "q_out"), _stream_on(batch.device, stream)))
+
+
+def paged_plan8_bytes(batch: PagedBatch) -> int:
+    return int(lib().ooo_paged_plan8_bytes(batch.address)) if batch.eight else 0
+
+
+def paged_plan8(batch: PagedBatch, plan=None, stream=None):
+    """As ``paged_plan``, for ``paged_attn8``."""
+    import torch
+
+    if not batch.eight:
+        raise ValueError(f"the batch's pages hold {batch.pool_dtype}: not for this call")
+    if plan is None:
+        plan = torch.empty(max(paged_plan8_bytes(batch), 16), dtype=torch.uint8, device=batch.device)
+    _check(lib().ooo_paged_plan8(batch.address, _on(plan, "plan", batch.device, torch.uint8), plan.numel(),
+                                 _stream_on(batch.device, stream)))
+    return plan
+
+
+def paged_attn8_workspace(batch: PagedBatch) -> int:
+    return int(lib().ooo_paged_attn8_workspace(batch.address)) if batch.eight else 0
+
+
+def paged_attn8(batch: PagedBatch, cache: Cache8, plan, q, scale: float, out, workspace, layer: int = 0,
+                stream=None) -> None:
+    """As ``paged_attn``, over one layer of an 8-bit cache; plan of
+    ``paged_plan8``, workspace of ``paged_attn8_workspace`` bytes."""
+    import torch
+
+    ws = _on(workspace, "workspace", batch.device)
+    _check(lib().ooo_paged_attn8(batch.address, cache.of(batch), layer, _on(plan, "plan", batch.device, torch.uint8),
+                                 plan.numel(), batch.row_ptr(q, "q"), scale, batch.row_ptr(out, "out"), ws,
+                                 workspace.numel() * workspace.element_size(), _stream_on(batch.device, stream)))
+
+
+def paged_compact8(batch: PagedBatch, cache: Cache8, path, accept_len, stream=None) -> None:
+    """As ``paged_compact``, in all layers of an 8-bit cache."""
+    import torch
+
+    if path.dim() != 2:
+        raise ValueError("path must be [n_seqs][path_cap]")
+    cap = path.shape[1]
+    _check(lib().ooo_paged_compact8(batch.address, cache.of(batch),
+                                    _on(path, "path", batch.device, torch.int32, (batch.n_seqs, cap)),
+                                    _on(accept_len, "accept_len", batch.device, torch.int32, (batch.n_seqs,)), cap,
+                                    _stream_on(batch.device, stream)))
+
+
+def _fork_args(batch: PagedBatch, parent, fresh, seq_len_out, table_out):
+    import torch
+
+    i, n, ld = torch.int32, batch.n_seqs, batch.struct.table_ld
+    ptrs = [_on(parent, "parent", batch.device, i, (n,)), _on(fresh, "fresh", batch.device, i, (n,)),
+            _on(seq_len_out, "seq_len_out", batch.device, i, (n,)),
+            _on(table_out, "table_out", batch.device, i, (n, ld))]
+    for own, out, size, nm in ((batch.struct.seq_len, ptrs[2], 4 * n, "seq_len_out"),
+                               (batch.struct.page_table, ptrs[3], 4 * n * ld, "table_out")):
+        if own != out and own < out + size and out < own + size:
+            raise ValueError(f"{nm} overlaps the batch's own array")
+    return ptrs
+
+
+def paged_fork(batch: PagedBatch, k_pages, v_pages, parent, fresh, seq_len_out, table_out, stream=None) -> None:
+    """Sequences become continuations of others: k_pages/v_pages the pools of all
+    layers, [L][n_pages][Hkv][page_rows][D] (or one layer's); parent, fresh
+    [n_seqs] int32; seq_len_out [n_seqs], table_out [n_seqs][table_ld] int32: both
+    the batch's own tensors, or neither."""
+    if k_pages.dim() not in (4, 5) or k_pages.dim() != v_pages.dim() or k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages and v_pages must be [L][n_pages][n_kv_heads][page_rows][head_dim]")
+    many = k_pages.dim() == 5
+    if many and k_pages.stride(0) != v_pages.stride(0):
+        raise ValueError("k_pages and v_pages must have the same strides")
+    _check(lib().ooo_paged_fork(batch.address, batch.pool_ptr(k_pages, "k_pages"), batch.pool_ptr(v_pages, "v_pages"),
+                                k_pages.shape[0] if many else 1, k_pages.stride(0) if many else 0,
+                                *_fork_args(batch, parent, fresh, seq_len_out, table_out),
+                                _stream_on(batch.device, stream)))
+
+
+def paged_fork8(batch: PagedBatch, cache: Cache8, parent, fresh, seq_len_out, table_out, stream=None) -> None:
+    """As ``paged_fork``, in all layers of an 8-bit cache."""
+    _check(lib().ooo_paged_fork8(batch.address, cache.of(batch),
+                                 *_fork_args(batch, parent, fresh, seq_len_out, table_out),
+                                 _stream_on(batch.device, stream)))
+
+
+# ----------------------------------------------------------------------------
+# sampling
 
 
 def sample_workspace(n_rows: int, vocab: int) -> int:
