@@ -28,16 +28,19 @@ __device__ __forceinline__ void dma4_nt(const void* base, uint32_t voff, uint32_
 }
 
 // LDS geometry of tiles of 8-bit rows: row-major, the 16-byte chunks of a row
-// permuted so that both the K reads (16 rows, one chunk) and the V transpose
-// reads (8 rows, two chunks) lie in distinct banks.
+// permuted so that the reads of K (16 rows and one chunk: sixteen in a row, or
+// four of every eight) and the transpose reads of V (8 rows and two chunks, or
+// 16 rows and one) lie in distinct banks.
 template <int D>
 struct Ring8 {
   static constexpr int CH = D / 16;         // chunks of a row
   static constexpr int MAT = kTile * D;     // bytes of a tile of K or V
   static constexpr int HALF = 32 * D;       // of a half-tile, the rows of one scale
   static constexpr int BYTES = 128 * 1024;  // of the ring: 16 KiB a wave
+  static constexpr int FOURTH = D / 2;      // what four or 16 rows on turn in an address
   static __device__ __forceinline__ int swz(int r, int c) {
-    return c ^ (D == 128 ? (r & 6) | ((r >> 3) & 1) : ((r >> 1) & 2) | ((r >> 3) & 1));
+    const int x = (r >> 3) & 1, y = ((r >> 2) ^ (r >> 4)) & 1;
+    return c ^ (D == 128 ? x | (r & 2) | y << 2 : x | y << 1);
   }
 };
 
@@ -54,14 +57,14 @@ struct Window8 {
   long long stride, head, scale_stride, scale_head;
   int k0, step, last, count, shift, n_pages, lane, row_bytes;
   uint8_t* buf;
-  int base, sbase;
+  int base, kbase, vbase;
   uint32_t lo, hi, lds, kx, vx;
   bool bad;
   __device__ __forceinline__ int key(int n) const { return min(k0 + n * step, last); }
   __device__ __forceinline__ void start() {
     lds = __builtin_amdgcn_readfirstlane(lds_addr(buf));
     base = 0;
-    sbase = -64;
+    kbase = vbase = -64;
     kx = vx = 0;
     bad = false;
     take(ids[key(lane) >> shift]);
@@ -100,21 +103,41 @@ struct Window8 {
     return (long long)((unsigned long long)(uint32_t)__builtin_amdgcn_readlane(hi, n - base) << 32 |
                        (uint32_t)__builtin_amdgcn_readlane(lo, n - base));
   }
-  // Before scale(n), for rising n, behind the wait for step n's keys.
-  __device__ __forceinline__ void turn_scales(int n) {
-    if (n - sbase < 64) return;
-    sbase += 64;
-    const uint32_t sh = *word(0, sbase);
-    kx = (*word(1, sbase) >> (sh & 31) & 255) << 23;
-    vx = (*word(2, sbase) >> (sh >> 8 & 31) & 255) << 23;
+  // The scale of step n's keys or values, for rising n, behind the wait for step
+  // n's keys.
+  __device__ __forceinline__ float k_scale(int n) {
+    if (n - kbase >= 64) {
+      kbase += 64;
+      kx = (*word(1, kbase) >> (*word(0, kbase) & 31) & 255) << 23;
+    }
+    return __uint_as_float(__builtin_amdgcn_readlane(kx, n & 63));
   }
-  __device__ __forceinline__ float k_scale(int n) const {
-    return __uint_as_float(__builtin_amdgcn_readlane(kx, n - sbase));
-  }
-  __device__ __forceinline__ float v_scale(int n) const {
-    return __uint_as_float(__builtin_amdgcn_readlane(vx, n - sbase));
+  __device__ __forceinline__ float v_scale(int n) {
+    if (n - vbase >= 64) {
+      vbase += 64;
+      vx = (*word(2, vbase) >> (*word(0, vbase) >> 8 & 31) & 255) << 23;
+    }
+    return __uint_as_float(__builtin_amdgcn_readlane(vx, n & 63));
   }
 };
+
+// Waits until only `ahead` (0 .. MOST) times PER and EXTRA requests are on their way.
+template <int PER, int EXTRA, int MOST>
+__device__ __forceinline__ void wait_ahead(int ahead) {
+  if constexpr (MOST == 0) {
+    wait_vmcnt<EXTRA>();
+  } else {
+    if (ahead >= MOST) wait_vmcnt<MOST * PER + EXTRA>();
+    else wait_ahead<PER, EXTRA, MOST - 1>(ahead);
+  }
+}
+
+// D = A(16x32) * B(32x16) + C with bf16 inputs and float32 accumulation.  Lane l
+// holds A row (l % 16), k = 8*(l/16) .. +8; B column (l % 16), same k range; C/D
+// element (row 4*(l/16) + r, column l % 16) in r.
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
 // Eight numbers times a power of two.
 __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float up) {
@@ -124,6 +147,61 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float up) {
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, up, true))});
 }
 
+// The steps of an item, 32 keys each, from key k0 on.
+template <int D>
+__device__ __forceinline__ Window8 window_of(const PagedAttnArgs& a, const Item& it, int g, int lane, int k0, int step,
+                                             uint8_t* buf) {
+  Window8 w;
+  w.ids = it.flags & kShared ? a.p.shared_pages : a.p.table + (size_t)it.seq * a.p.table_ld;
+  w.ks = a.c.scales[0];
+  w.vs = a.c.scales[1];
+  w.stride = a.p.page_stride;
+  w.head = ((long long)g << a.p.page_shift) * D;
+  w.scale_stride = a.c.scale_stride;
+  w.scale_head = (long long)g * a.c.page_blocks;
+  w.k0 = k0;
+  w.step = step;
+  w.last = it.limit - 1;
+  w.count = it.t1 - it.t0;
+  w.shift = a.p.page_shift;
+  w.n_pages = a.p.n_pages;
+  w.lane = lane;
+  w.row_bytes = D;
+  w.buf = buf;
+  return w;
+}
+
+// The copies of a wave that works on half-tiles alone: its share of the ring is
+// NS stages of a K half-tile and one of V.
+template <int D>
+struct HalfCopy {
+  using R = Ring8<D>;
+  static constexpr int HI = R::HALF / 1024;            // DMA instructions of a half-tile
+  static constexpr int NS = 16384 / (2 * R::HALF);
+  static constexpr int RPI = 1024 / D;                 // rows of an instruction
+  uint32_t full[HI];
+  int lane, keys;  // from the item's first on
+  __device__ __forceinline__ HalfCopy(const Item& it, int ln) : lane(ln), keys(it.limit - 32 * it.t0) {
+#pragma unroll
+    for (int x = 0; x < HI; ++x) full[x] = off(x, 31);
+  }
+  // From the half-tile's first row to a lane's source; rows past `last` repeat it.
+  __device__ __forceinline__ uint32_t off(int x, int last) const {
+    const int r = x * RPI + lane / R::CH;
+    return (uint32_t)min(r, last) * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
+  }
+  __device__ __forceinline__ void operator()(const uint8_t* src, int n, uint32_t to) const {
+    const int last = keys - 32 * n - 1;
+    if (last >= 31) {
+#pragma unroll
+      for (int x = 0; x < HI; ++x) dma16_nt(src, full[x], to + x * 1024);
+    } else {
+#pragma unroll
+      for (int x = 0; x < HI; ++x) dma16_nt(src, off(x, last), to + x * 1024);
+    }
+  }
+};
+
 // One item by a workgroup (WIDE; every wave calls it) or by a wave alone.
 template <int D, bool NEG, bool WIDE>
 __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int wave, uint8_t* ring,
@@ -131,8 +209,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   using R = Ring8<D>;
   constexpr int NW = kPagedWaves, RG = 4, NP = D / 8, DT = D / 32, S = D / 16;
   constexpr int V0 = 4 * R::MAT;       // of a wide ring: four stages of K, then of V
-  constexpr int HI = R::HALF / 1024;   // DMA instructions of a half-tile
-  constexpr int NS = 16384 / (2 * R::HALF);  // stages of a narrow wave
+  constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS;
   constexpr int kJoinMl = RG * NP * 64 * 16;  // where the joined halves' statistics lie, behind their sums
   static_assert(8 * R::MAT <= R::BYTES && kJoinMl + RG * 64 * 8 <= R::BYTES, "ring");
   const PagedAttnArgs& a = args_again();
@@ -154,23 +231,8 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
 #pragma unroll
     for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(ld16(qrow + 16 * (2 * (x / 2) + u) + 8 * (x & 1)));
   }
-  Window8 window;
-  window.ids = it.flags & kShared ? p.shared_pages : p.table + (size_t)it.seq * p.table_ld;
-  window.ks = a.c.scales[0];
-  window.vs = a.c.scales[1];
-  window.stride = p.page_stride;
-  window.head = ((long long)g << p.page_shift) * D;
-  window.scale_stride = a.c.scale_stride;
-  window.scale_head = (long long)g * a.c.page_blocks;
-  window.k0 = WIDE ? kTileKeys * it.t0 + 32 * kh0 : 32 * it.t0;
-  window.step = WIDE ? kTileKeys : 32;
-  window.last = it.limit - 1;
-  window.count = it.t1 - it.t0;
-  window.shift = p.page_shift;
-  window.n_pages = p.n_pages;
-  window.lane = lane;
-  window.row_bytes = D;
-  window.buf = windows + wave * Window8::BYTES;
+  Window8 window = window_of<D>(a, it, g, lane, WIDE ? kTileKeys * it.t0 + 32 * kh0 : 32 * it.t0,
+                                WIDE ? kTileKeys : 32, windows + wave * Window8::BYTES);
   window.start();
   const int all = all_see(p, it);
   const uint8_t* const kp = (const uint8_t*)a.k;
@@ -179,7 +241,8 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   // LDS addresses of the fragments in the wave's first stage.  K read j: chunk
   // 2 j + u of row sigma(c), 32 j bytes away by the permutation's exclusive or.
   // V transpose read (16 keys kk, column block dt): row 16 kk + 8 (g16 / 2) +
-  // li / 2, chunk 2 dt + g16 % 2, its half li % 2: 32 dt bytes away.
+  // li / 2, chunk 2 dt + g16 % 2, its half li % 2: 32 dt bytes away, and kk turns
+  // the permutation's bit of row 16.
   const uint32_t k_lds = lds_addr(ring) + (WIDE ? kh0 * R::HALF : wave * 16384);
   const uint32_t v_lds = k_lds + (WIDE ? V0 : R::HALF);
   const int krow = sigma(c), g16 = lane >> 4, li = lane & 15;
@@ -224,7 +287,8 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   auto vread = [&](int x) OOO_INLINE {  // 16 keys x / DT, column block x % DT
     return __builtin_bit_cast(
         u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                   (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32u * (x % DT))) + 16 * (x / DT) * D)));
+                   (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32u * (x % DT)) ^ (uint32_t)(R::FOURTH * (x / DT))) +
+                                                                         16 * (x / DT) * D)));
   };
   auto pv = [&](int x, const u32x2& v, float up, const bf16x8 (&pr)[2]) OOO_INLINE {
     oacc[x % DT] = mfma32(bf16_of(v[0], v[1], up), pr[x / DT], oacc[x % DT]);
@@ -309,92 +373,211 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
     const uint64_t* const words = mwords + qr * p.W;
     // A wave copies rows 8 wave .. 8 wave + 7 of every tile, which lie in its own
     // half: 1 KiB at head_dim 128 (16 bytes a lane), 512 bytes at 64 (4 bytes, twice).
+    constexpr int PM = D == 128 ? 1 : 2;  // DMA instructions of a wave for K or V of a tile
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(ring) + wave * 8 * D);
-    auto copy = [&](const uint8_t* pool, int n, uint32_t to) OOO_INLINE {
-      const uint8_t* const src = pool + window.at(n);
-      const int end = it.limit - kTileKeys * (it.t0 + n) - 1;  // rows past the last one repeat it
+    // from the half's first row in its page to a lane's source; rows past `last` repeat it
+    auto rows_off = [&](int x, int last) OOO_INLINE -> uint32_t {
       if constexpr (D == 128) {
         const int r = 8 * wave + lane / 8;
-        dma16_nt(src, (uint32_t)(min(r, end) & 31) * D + (uint32_t)R::swz(r, lane % 8) * 16u, to);
+        return (uint32_t)(min(r, last) & 31) * D + (uint32_t)R::swz(r, lane % 8) * 16u;
       } else {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int r = 8 * wave + 4 * x + lane / 16;
-          dma4_nt(src, (uint32_t)(min(r, end) & 31) * D + (uint32_t)R::swz(r, lane % 16 / 4) * 16u + lane % 4 * 4u,
-                  to + x * 256);
-        }
+        const int r = 8 * wave + 4 * x + lane / 16;
+        return (uint32_t)(min(r, last) & 31) * D + (uint32_t)R::swz(r, lane % 16 / 4) * 16u + lane % 4 * 4u;
       }
     };
-    queries_here();
-    for (int n = 0; n < tiles; ++n) {
-      window.turn(n);
+    auto copy1 = [&](const uint8_t* src, uint32_t off, uint32_t to, int x) OOO_INLINE {
+      if constexpr (D == 128) dma16_nt(src, off, to);
+      else dma4_nt(src, off, to + x * 256);
+    };
+    uint32_t full_off[PM];
+#pragma unroll
+    for (int x = 0; x < PM; ++x) full_off[x] = rows_off(x, 63);
+    auto stage = [&](int n) OOO_INLINE -> uint32_t { return (uint32_t)(n & 3) * R::MAT; };
+    const int full = min(tiles, (it.limit >> 6) - it.t0);  // tiles whose keys all exist
+    auto copy_full = [&](const uint8_t* src, uint32_t to, int x) OOO_INLINE {
+      if (x < PM) copy1(src, full_off[x], to, x);
+    };
+    auto copy = [&](const uint8_t* src, int n, uint32_t to) OOO_INLINE {
+      if (n < full) {
+        copy_full(src, to, 0);
+        copy_full(src, to, 1);
+      } else if (n < tiles) {
+#pragma unroll
+        for (int x = 0; x < PM; ++x) copy1(src, rows_off(x, it.limit - kTileKeys * (it.t0 + n) - 1), to, x);
+      }
+    };
+    // The order of copies, barriers and blocks is the bf16 kernel's.  Barrier m
+    // says that K of tile m and V of tile m - 1 are here and that nobody reads K
+    // of tile m - 1 or V of tile m - 3 any more.  Between it and the next, V of
+    // tile m + 1 and K of tile m + 3 are asked for; where V lies is remembered
+    // from K.
+    long long src[3] = {0, 0, 0};  // of K of the three youngest tiles, the last one first
+    auto aim = [&](int n) OOO_INLINE {
+      src[2] = src[1];
+      src[1] = src[0];
+      src[0] = window.at(n);
+    };
+    auto ask_k = [&](int n) OOO_INLINE {
+      if (n < tiles) window.turn(n);
+      aim(min(n, tiles - 1));
+      copy(kp + src[0], n, dst + stage(n));
+    };
+    auto ask_v = [&](int n, int back) OOO_INLINE { copy(vp + src[back], n, dst + V0 + stage(n)); };
+    auto barrier = [&](int m) OOO_INLINE {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      wg_barrier();  // nobody reads the tile before
-      copy(kp, n, dst);
-      copy(vp, n, dst + V0);
-      wait_vmcnt<0>();
+      if (m + 2 < tiles) wait_vmcnt<2 * PM>();  // K of m + 2 and V of m may be on their way
+      else if (m < tiles) wait_vmcnt<PM>();
+      else wait_vmcnt<0>();
       wg_barrier();
-      if (idle) continue;
-      window.turn_scales(n);
+    };
+    auto to_next = [&](int n) OOO_INLINE -> uint32_t {  // from the stage of tile n to that of n + 1
+      return (n & 3) == 3 ? (uint32_t)(-3 * R::MAT) : (uint32_t)R::MAT;
+    };
+    queries_here();
+    ask_k(0);
+    ask_k(1);
+    ask_v(0, 1);
+    ask_k(2);
+    barrier(0);
+    if (idle) {  // copies and keeps step
+#pragma unroll 1
+      for (int m = 1; m <= tiles + 1; ++m) {
+        ask_v(m, 1);
+        ask_k(m + 2);
+        barrier(m);
+      }
+    } else {
+      // A tile is a block of vector work, the softmax of tile n, with the
+      // products of the scores of tile n + 1 and the reads of V of tile n between,
+      // and one of the products P V of tile n with the reads of K of tile n + 2
+      // between.  Wave A (kh0 = 0) has its barrier between the two, wave B before
+      // the first, so that the blocks of the two alternate on a SIMD.  The first
+      // block asks for V, of tile n + 2 by A and n + 3 by B, the second for K of
+      // tile n + 5.  Tiles whose keys all rows see and whose copies need no care go
+      // through a body without conditions.
       u32x4 kr[DT];
-      u32x2 vv[S];
+      u32x2 vr[S];
       bf16x8 pf[2];
       kread(kr);
-      f32x16 sc = scores(kr, window.k_scale(n));
-      masked(sc, kTileKeys * (it.t0 + n) + 32 * kh0, words);
-      settle(sc);
-      weights(sc, new_max(row_max(sc, []() {})), pf, [](int) {});
+      ask_v(1, 1);
+      ask_k(3);
+      f32x16 sc = scores(kr, window.k_scale(0));
+      barrier(1);
+      k_at += to_next(0);
+      kread(kr);
+      if (kh0 == 1) ask_v(2, 1);
+      ask_k(4);
+      auto tile = [&](auto plain, int n) OOO_INLINE {
+        constexpr bool PLAIN = decltype(plain)::value;
+        auto turn = [&]() OOO_INLINE {
+          if constexpr (PLAIN) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_vmcnt<2 * PM>();
+            wg_barrier();
+          } else {
+            barrier(n + 2);
+          }
+        };
+        const float k_up = window.k_scale(n + 1 < tiles ? n + 1 : n), v_up = window.v_scale(n);
+        if (kh0 == 1) turn();
+        f32x16 next = score1(0, kr, k_up, f32x16{});
+        const int nv = n + 2 + kh0;
+        const uint8_t* const v_src = vp + (kh0 == 0 ? src[2] : src[1]);
+        const uint32_t v_to = dst + V0 + stage(nv);
+        if constexpr (!PLAIN) {
+          masked(sc, kTileKeys * (it.t0 + n) + 32 * kh0, words);
+          copy(v_src, nv, v_to);
+        }
+        settle(sc);
+        const float m_use = new_max(row_max(sc, [&]() OOO_INLINE {
+          __builtin_amdgcn_sched_barrier(0);
+          next = score1(1, kr, k_up, next);
+          __builtin_amdgcn_sched_barrier(0);
+        }));
+        weights(sc, m_use, pf, [&](int k) OOO_INLINE {
+          if (k + 2 < S) next = score1(k + 2, kr, k_up, next);
+          if (k < S) vr[k] = vread(k);
+          if (PLAIN && k == 2) copy_full(v_src, v_to, 0);
+          if (PLAIN && k == 5) copy_full(v_src, v_to, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        v_at += to_next(n);
+        // else the compiler moves them to their use, behind wave A's barrier
+        asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(l_run));
+        if (kh0 == 0) turn();
+        k_at += to_next(n + 1);
+        if constexpr (PLAIN) aim(min(n + 5, tiles - 1));  // the last one again where there is none
+        else ask_k(n + 5);
+        const uint32_t k_to = dst + stage(n + 5);
 #pragma unroll
-      for (int x = 0; x < S; ++x) vv[x] = vread(x);
-      const float up = window.v_scale(n);
-#pragma unroll
-      for (int x = 0; x < S; ++x) pv(x, vv[x], up, pf);
+        for (int x = 0; x < S; ++x) {
+          pv(x, vr[x], v_up, pf);
+          if (x % 2 == 0) kr[x / 2] = kread1(x / 2);
+          if (PLAIN && x == S / 4) copy_full(kp + src[0], k_to, 0);
+          if (PLAIN && x == S - S / 4) copy_full(kp + src[0], k_to, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sc = next;
+      };
+      for (int n = 0; n < tiles; ++n) {
+        // the plain tiles end at the first that some row does not see all of, and
+        // five before one that is not full or begins a window
+        const int care = min(full, window.base + 64);
+        int end = min(tiles, (all >> 6) - it.t0);
+        if (care < tiles) end = min(end, care - 5);
+#pragma unroll 1
+        for (; n < end; ++n) tile(Yes{}, n);
+        if (n < tiles) tile(No{}, n);
+      }
     }
   } else {
-    const uint32_t kd = __builtin_amdgcn_readfirstlane(k_lds), vd = kd + R::HALF;
-    uint32_t full_off[HI];
-    const int rpi = 1024 / D;
-#pragma unroll
-    for (int x = 0; x < HI; ++x) {
-      const int r = x * rpi + lane / R::CH;
-      full_off[x] = (uint32_t)r * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
-    }
-    auto ask = [&](const uint8_t* pool, int n, uint32_t dst) OOO_INLINE {
-      const uint8_t* const src = pool + window.at(n);
-      const int end = it.limit - 32 * (it.t0 + n) - 1;
-#pragma unroll
-      for (int x = 0; x < HI; ++x) {
-        uint32_t off = full_off[x];
-        if (end < 31) {
-          const int r = x * rpi + lane / R::CH;
-          off = (uint32_t)min(r, end) * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
-        }
-        dma16_nt(src, off, dst + x * 1024);
-      }
-    };
-    const uint64_t* const words = p.mask + (size_t)row * p.W;
+    // The wave's share of the ring: NS stages of a K half-tile and one of V.  A
+    // half-tile is read into registers whole, K, then V, so that the one NS steps
+    // on is asked for before the work on it begins.
+    const uint32_t kd = __builtin_amdgcn_readfirstlane(k_lds);
+    const HalfCopy<D> copy(it, lane);
     const int count = it.t1 - it.t0;
+    const uint64_t* const words = p.mask + (size_t)row * p.W;
     queries_here();
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+      if (n < count) {
+        copy(kp + window.at(n), n, kd + n * 2 * R::HALF);
+        copy(vp + window.at(n), n, kd + n * 2 * R::HALF + R::HALF);
+      }
     for (int n = 0; n < count; ++n) {
-      window.turn(n);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      ask(kp, n, kd);
-      ask(vp, n, vd);
-      wait_vmcnt<0>();
-      window.turn_scales(n);
+      const uint32_t st = kd + (uint32_t)(n % NS) * 2 * R::HALF;
+      const int ahead = min(count - 1 - n, NS - 1);  // later half-tiles on their way, K and V
+      const bool more = n + NS < count;
       u32x4 kr[DT];
-      u32x2 vv[S];
+      u32x2 vr[S];
       bf16x8 pf[2];
+      wait_ahead<2 * HI, HI, NS - 1>(ahead);
+      const float k_up = window.k_scale(n);
       kread(kr);
-      f32x16 sc = scores(kr, window.k_scale(n));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      long long src = 0;
+      if (more) {
+        window.turn(n + NS);
+        src = window.at(n + NS);
+        copy(kp + src, n + NS, st);
+      }
+      f32x16 sc = scores(kr, k_up);
       masked(sc, 32 * (it.t0 + n), words);
       settle(sc);
       weights(sc, new_max(row_max(sc, []() {})), pf, [](int) {});
+      if (more) wait_vmcnt<(NS - 1) * 2 * HI + HI>();
+      else wait_ahead<2 * HI, 0, NS - 1>(ahead);
+      const float v_up = window.v_scale(n);
 #pragma unroll
-      for (int x = 0; x < S; ++x) vv[x] = vread(x);
-      const float up = window.v_scale(n);
+      for (int x = 0; x < S; ++x) vr[x] = vread(x);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (more) copy(vp + src, n + NS, st + R::HALF);
+      const uint32_t step = n % NS == NS - 1 ? (uint32_t)(-2 * (NS - 1) * R::HALF) : (uint32_t)(2 * R::HALF);
+      k_at += step;
+      v_at += step;
 #pragma unroll
-      for (int x = 0; x < S; ++x) pv(x, vv[x], up, pf);
+      for (int x = 0; x < S; ++x) pv(x, vr[x], v_up, pf);
     }
   }
   bool bad = window.bad;
@@ -525,6 +708,217 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   }
 }
 
+// One item of up to 16 query rows by a wave alone: decoding, where a sequence has
+// one row for each query head of the group.  On 16x16x32 products it costs half
+// the matrix and softmax work of the narrow item above, which leaves the copies.
+// S^T = K Q^T in two blocks of 16 keys, of which block t's row i is key 8 (i / 4)
+// + 4 t + i % 4, so that lane (c, u) holds row c's keys 8 u .. 8 u + 7 in operand
+// order; O^T = V^T P^T in blocks of 16 columns: columns 16 dt + 4 u + 0..3.
+template <int D, bool NEG>
+__device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int wave, uint8_t* ring,
+                                                 uint8_t* windows) {
+  using R = Ring8<D>;
+  constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS, S = D / 32, DT = D / 16;
+  const PagedAttnArgs& a = args_again();
+  const Paged p = a.p;
+  const float scale = a.scale_log2e;
+  const Item it = load_item(a.plan + a.off_items_n, item);
+  const int c = lane & 15, u = lane >> 4;
+  const int qi = it.q0 + min(c, it.nq - 1), i = qi / p.G, hq = g * p.G + qi - i * p.G;
+  const long long row = (long long)it.row0 + i;
+  bf16x8 qf[S];  // products 2 j and 2 j + 1 take a key's 16 columns 16 (4 j + u) on
+  {
+    const uint16_t* qrow = (const uint16_t*)a.q + (row * p.Hq + hq) * D;
+#pragma unroll
+    for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(ld16(qrow + 16 * (4 * (x / 2) + u) + 8 * (x & 1)));
+  }
+  Window8 window = window_of<D>(a, it, g, lane, 32 * it.t0, 32, windows + wave * Window8::BYTES);
+  window.start();
+  const int all = all_see(p, it);
+  const uint8_t* const kp = (const uint8_t*)a.k;
+  const uint8_t* const vp = (const uint8_t*)a.v;
+  const uint32_t kd = __builtin_amdgcn_readfirstlane(lds_addr(ring) + wave * 16384);
+  const int krow = 8 * (c >> 2) + (c & 3), vrow = 8 * u + (c >> 1);
+  uint32_t k_at = kd + krow * D + (R::swz(krow, u) << 4);
+  uint32_t v_at = kd + R::HALF + vrow * D + (R::swz(vrow, 0) << 4) + 8 * (c & 1);
+#pragma unroll
+  for (int x = 0; x < S; ++x) asm volatile("" : "+v"(qf[x]));  // here, not inside the loop
+  if constexpr (NEG) {
+#pragma unroll
+    for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(__builtin_bit_cast(u32x4, qf[x]) ^ 0x80008000u);
+  }
+  f32x4 oacc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+  const HalfCopy<D> copy(it, lane);
+  const int count = it.t1 - it.t0;
+  const uint64_t* const words = p.mask + (size_t)row * p.W;
+#pragma unroll
+  for (int n = 0; n < NS; ++n)
+    if (n < count) {
+      copy(kp + window.at(n), n, kd + n * 2 * R::HALF);
+      copy(vp + window.at(n), n, kd + n * 2 * R::HALF + R::HALF);
+    }
+  for (int n = 0; n < count; ++n) {
+    const uint32_t st = kd + (uint32_t)(n % NS) * 2 * R::HALF;
+    const int ahead = min(count - 1 - n, NS - 1);
+    const bool more = n + NS < count;
+    u32x4 kr[2][D / 64];
+    u32x2 vr[DT];
+    wait_ahead<2 * HI, HI, NS - 1>(ahead);
+    const float k_up = window.k_scale(n);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j)
+        kr[t][j] = *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)((k_at ^ (64u * j) ^
+                                                                                 (uint32_t)(R::FOURTH * t)) +
+                                                                                4 * t * D);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    long long src = 0;
+    if (more) {
+      window.turn(n + NS);
+      src = window.at(n + NS);
+      copy(kp + src, n + NS, st);
+    }
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int x = 0; x < S; ++x)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = mfma16(bf16_of(kr[t][x / 2][2 * (x & 1)], kr[t][x / 2][2 * (x & 1) + 1], k_up), qf[x], s[t]);
+    const int lo = 32 * (it.t0 + n);
+    if (lo + 32 > all) {
+      const uint32_t b = (uint32_t)seen_in(p, it, i, words, lo) >> (8 * u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!((b >> j) & 1u)) s[j / 4][j % 4] = -INFINITY;
+    }
+    {  // as settle()
+      const int x = __builtin_amdgcn_readfirstlane(__float_as_int(s[1][3]));
+      asm volatile("" : "+v"(s[0]), "+v"(s[1]) : "s"(x));
+    }
+    float mx = max3f(max3f(s[0][0], s[0][1], s[0][2]), max3f(s[1][0], s[1][1], s[1][2]), max3f(s[0][3], s[1][3], -INFINITY));
+    {
+      const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = max3f(__uint_as_float(h[0]), __uint_as_float(h[1]), -INFINITY);
+      const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = max3f(__uint_as_float(q[0]), __uint_as_float(q[1]), -INFINITY) * scale;
+    }
+    if (__any(mx > m_run + 8.f)) {
+      const float m_new = __builtin_fmaxf(m_run, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    u32x4 pk;
+    float ps[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[j / 2][2 * (j & 1)], scale, -m_use));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[j / 2][2 * (j & 1) + 1], scale, -m_use));
+      pk[j] = pack_bf16x2(e0, e1);
+      ps[j & 1] = add_bf16x2(pk[j], ps[j & 1]);
+    }
+    l_run += ps[0] + ps[1];
+    const bf16x8 pf = as_bf16x8(pk);
+    if (more) wait_vmcnt<(NS - 1) * 2 * HI + HI>();
+    else wait_ahead<2 * HI, 0, NS - 1>(ahead);
+    const float v_up = window.v_scale(n);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      vr[dt] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                             (i32x2 __attribute__((address_space(3)))*)(uintptr_t)(v_at ^ (16u * dt))));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) copy(vp + src, n + NS, st + R::HALF);
+    const uint32_t step = n % NS == NS - 1 ? (uint32_t)(-2 * (NS - 1) * R::HALF) : (uint32_t)(2 * R::HALF);
+    k_at += step;
+    v_at += step;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = mfma16(bf16_of(vr[dt][0], vr[dt][1], v_up), pf, oacc[dt]);
+  }
+  bool bad = window.bad;
+
+  const PagedAttnArgs& ea = args_again();
+  const Paged& ep = ea.p;
+  const Item e = load_item(ea.plan + ea.off_items_n, item);
+  const int eq = e.q0 + min(c, e.nq - 1), ei = eq / ep.G;
+  const long long row_e = (long long)e.row0 + ei;
+  const auto whole = [](float x) { return (x + shfl_xor_f(x, 16)) + shfl_xor_f(x + shfl_xor_f(x, 16), 32); };
+
+  // Sums that are not finite though the weights are: the keys once more, without
+  // those of weight zero (paged_attn8_item).
+  float z = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z = __builtin_fmaf(oacc[dt][j], 0.f, z);
+  bool again = __any(!(z == 0.f));
+  if (again) again = __any(!(z == 0.f) && whole(l_run) < INFINITY);
+  if (again) {
+    const Pages pages(ep, e);
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    l_run = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int h = e.t0; h < e.t1; ++h) {
+      const uint64_t bits = seen(ep, e, ei, (int)row_e, 32 * h);
+#pragma unroll 1
+      for (int j = 0; j < 32 && 32 * h + j < e.limit; ++j) {
+        const int t = 32 * h + j;
+        const int page = pages.at(t, bad), pr = t & ((1 << ep.page_shift) - 1);
+        const long long base = (long long)page * ep.page_stride + (((long long)g << ep.page_shift) + pr) * D;
+        const long long so = (long long)page * ea.c.scale_stride + (long long)g * ea.c.page_blocks + pr / kBlockRows;
+        const float ku = scale_of(ea.c.scales[0] + so), vu = scale_of(ea.c.scales[1] + so);
+        float s = 0.f;
+#pragma unroll
+        for (int y = 0; y < D / 64; ++y) {
+          const u32x4 kk = ld16((const uint8_t*)ea.k + base + 16 * (4 * y + u));
+#pragma unroll
+          for (int h2 = 0; h2 < 2; ++h2) {
+            const bf16x8 kb = bf16_of(kk[2 * h2], kk[2 * h2 + 1], ku);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s = __builtin_fmaf((float)kb[x], (float)qf[2 * y + h2][x], s);
+          }
+        }
+        s = whole(s);
+        const float w = (bits >> j) & 1 ? __builtin_amdgcn_exp2f(fmaf(s, ea.scale_log2e, -m_use)) : 0.f;
+        if (w == 0.f) continue;
+        if (u == 0) l_run += w;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          float x[4];
+          values4(*reinterpret_cast<const uint32_t*>((const uint8_t*)ea.v + base + 16 * dt + 4 * u), vu, x);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) oacc[dt][y] += w * x[y];
+        }
+      }
+    }
+  }
+  float l_tot = whole(l_run);
+  const bool direct = e.flags & kDirect;
+  if (c >= e.nq || (!direct && e.slot >= ea.max_slots)) return;
+  if (bad) l_tot = __builtin_nanf("");
+  if (direct) {
+    const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // a row that sees no key is zero
+    uint16_t* const orow = (uint16_t*)ea.out + (row_e * ep.Hq + g * ep.G + eq - ei * ep.G) * D + 4 * u;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      *reinterpret_cast<u32x2*>(orow + 16 * dt) = u32x2{pack_bf16x2(oacc[dt][0] * inv, oacc[dt][1] * inv),
+                                                        pack_bf16x2(oacc[dt][2] * inv, oacc[dt][3] * inv)};
+  } else {  // in the order of the narrow item's pieces
+    const size_t sl = (size_t)e.slot * ep.Hkv + g;
+    f32x4* const po = reinterpret_cast<f32x4*>(ea.part_o) + sl * (D / 8) * 64 + (u >> 1) * 64 + (u & 1) * 32 + c;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) po[2 * dt * 64] = oacc[dt];
+    if (u == 0) reinterpret_cast<f32x2_t*>(ea.part_ml)[sl * 32 + c] = f32x2_t{m_run, l_tot};
+  }
+}
+
 template <int D, bool NEG>
 __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttnArgs) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[Ring8<D>::BYTES];
@@ -550,8 +944,12 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn
   if (head.narrow_first == 0) __syncthreads();  // it may have done wide items
   const ScalarPtr fn = scalar_ptr(a.plan + a.off_first_n) + narrow * kPagedWaves + wave;
   const int n0 = fn[0], n1 = min(fn[1], a.max_items_n);
-  for (int item = n0; item < n1; ++item)
-    paged_attn8_item<D, NEG, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+  for (int item = n0; item < n1; ++item) {
+    if (load_item(a.plan + a.off_items_n, item).nq <= 16)
+      paged_attn8_thin<D, NEG>(item, g, lane, wave, ring, windows);
+    else
+      paged_attn8_item<D, NEG, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+  }
 }
 
 }  // namespace ooo
