@@ -10,11 +10,14 @@
 #include "rope.h"
 #include "vec16.h"
 
+#include <algorithm>
+
 namespace ooo {
 namespace {
 
 // ----------------------------------------------------------------- append
 constexpr int kAppendWaves = 4;
+constexpr int kFewRows = 4096;  // up to so many, a block's heads are shared out
 
 // The place of a new row (0 <= r < R: rows_of): its sequence, index in it, own
 // token and page (-1: it has none).
@@ -144,13 +147,14 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, int r0, int 
 }
 
 // The new rows r0 .. r0 + m - 1 of one sequence that lie in one block, at block
-// row `row` of block `blk` of the page.  A wave takes one head's K or V: its
-// rows (8 or 4 at a time) stay in registers while their largest size, and so
-// the scale, is found.  One row alone (decoding): a wave takes as many heads at
-// once.  `held`: block rows below `row` that are committed.
+// row `row` of block `blk` of the page.  A wave takes one head's K or V (task
+// kv Hkv + g): its rows (8 or 4 at a time) stay in registers while their largest
+// size, and so the scale, is found.  One row alone (decoding): a wave takes as
+// many heads at once (task kv groups + group).  `held`: block rows below `row`
+// that are committed.
 template <class T, int D>
-__device__ __forceinline__ void append_block(const AppendArgs& a, int r0, int m, int page, int blk, int row, bool held,
-                                             int lane, int wave, const float* cs_s, const float* sn_s) {
+__device__ __forceinline__ void append_block(const AppendArgs& a, int task, int r0, int m, int page, int blk, int row,
+                                             bool held, int lane, const float* cs_s, const float* sn_s) {
   using V = Vec16<T>;
   constexpr int N = V::N, HALF = D / 2, LPH = HALF / N, SLOTS = 64 / LPH, STEPS = kBlockRows / SLOTS;
   const Paged& p = a.p;
@@ -176,9 +180,9 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int r0, int m,
     }
   };
   if (m == 1) {
-    const int groups = (p.Hkv + SLOTS - 1) / SLOTS;
-    for (int t = wave; t < 2 * groups; t += kAppendWaves) {
-      const int kv = t >= groups, g0 = (t - kv * groups) * SLOTS, g = g0 + s;
+    {
+      const int groups = (p.Hkv + SLOTS - 1) / SLOTS;
+      const int kv = task >= groups, g0 = (task - kv * groups) * SLOTS, g = g0 + s;
       Half<T> x;
       load(x, 0, min(g, p.Hkv - 1), kv);
       const int was = held ? (int)*scale_at(kv, min(g, p.Hkv - 1)) - 127 : kLeastExp;
@@ -206,8 +210,8 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int r0, int m,
     }
     return;
   }
-  for (int t = wave; t < 2 * p.Hkv; t += kAppendWaves) {
-    const int kv = t >= p.Hkv, g = t - kv * p.Hkv;
+  {
+    const int kv = task >= p.Hkv, g = task - kv * p.Hkv;
     Half<T> x[STEPS];
 #pragma unroll
     for (int k = 0; k < STEPS; ++k) load(x[k], min(k * SLOTS + s, m - 1), g, kv);
@@ -241,19 +245,24 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int r0, int m,
 
 // Workgroups blockIdx.x < `units` go over the rows from span blockIdx.x on and
 // quantise the blocks that begin there (with a sequence's first new row, or a
-// block of its own tokens); the others take four rows of queries each.
+// block of its own tokens); the others take four rows of queries each.  Up to
+// kFewRows rows a block's heads go to several workgroups (blockIdx.y), four
+// heads' K or V each: 8 tries of 64 rows took 17.7 us with all heads in one, and
+// take 13.4 so; 10k rows of prompts take 51 with all in one and 59 so.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a, int units) {
-  constexpr int HALF = D / 2;
+  constexpr int HALF = D / 2, SLOTS = 64 / (HALF / Vec16<T>::N);
   __shared__ __attribute__((aligned(16))) float cs_s[kBlockRows * HALF], sn_s[kBlockRows * HALF];
   const Paged& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x >= units) {
-    append_queries<T, D>(a, ((int)blockIdx.x - units) * kAppendWaves, lane, wave, cs_s, sn_s);
+    if (blockIdx.y == 0)
+      append_queries<T, D>(a, ((int)blockIdx.x - units) * kAppendWaves, lane, wave, cs_s, sn_s);
     return;
   }
   const int R = rows_of(p);
-  const int end = min(((int)blockIdx.x + 1) * a.span, R);
+  const int end = min(((int)blockIdx.x + 1) * a.span, R), first = (int)blockIdx.y * kAppendWaves;
+  const int stride = (int)gridDim.y * kAppendWaves;
   for (int r = (int)blockIdx.x * a.span; r < end;) {
     const Place at = place_of(p, r, R, nullptr, lane);
     if (at.i < 0 || at.i >= at.rows || at.len < 0 || at.slot >= p.own_cap) {
@@ -262,16 +271,20 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a
     }
     const int row = (int)(at.slot & (kBlockRows - 1));
     const int m = min(kBlockRows - row, at.rows - at.i);
-    if ((at.i == 0 || row == 0) && at.page >= 0) {
+    const int keys = m == 1 ? (p.Hkv + SLOTS - 1) / SLOTS : p.Hkv;  // tasks of K; as many of V
+    if ((at.i == 0 || row == 0) && at.page >= 0 && first < 2 * keys) {
       const int blk = (int)(at.slot & ((1 << p.page_shift) - 1)) / kBlockRows;
-      __syncthreads();  // the last block's angles are read
-      for (int e = threadIdx.x; e < m * HALF; e += 64 * kAppendWaves) {
-        const int i = e / HALF;
-        const int pos = p.shared_len + at.len + (a.depth ? a.depth[r + i] : at.i + i);
-        rope_sincos(pos, a.fr.f[e % HALF], sn_s[e], cs_s[e]);
+      if (first < keys) {
+        __syncthreads();  // the last block's angles are read
+        for (int e = threadIdx.x; e < m * HALF; e += 64 * kAppendWaves) {
+          const int i = e / HALF;
+          const int pos = p.shared_len + at.len + (a.depth ? a.depth[r + i] : at.i + i);
+          rope_sincos(pos, a.fr.f[e % HALF], sn_s[e], cs_s[e]);
+        }
+        __syncthreads();
       }
-      __syncthreads();
-      append_block<T, D>(a, r, m, at.page, blk, row, at.i == 0 && row > 0, lane, wave, cs_s, sn_s);
+      for (int t = first + wave; t < 2 * keys; t += stride)
+        append_block<T, D>(a, t, r, m, at.page, blk, row, at.i == 0 && row > 0, lane, cs_s, sn_s);
     }
     r += m;
   }
@@ -280,72 +293,96 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a
 template <class T, int D>
 void launch_append8(AppendArgs& a, hipStream_t st) {
   const int units = (a.p.n_rows + a.span - 1) / a.span, rows = (a.p.n_rows + kAppendWaves - 1) / kAppendWaves;
-  append8_kernel<T, D><<<units + rows, 64 * kAppendWaves, 0, st>>>(a, units);
+  const int tasks = a.p.n_rows > kFewRows ? 1 : (2 * a.p.Hkv + kAppendWaves - 1) / kAppendWaves;
+  append8_kernel<T, D><<<dim3(units + rows, tasks), 64 * kAppendWaves, 0, st>>>(a, units);
 }
 
-// ---------------------------------------------------------------- compact
-// One workgroup for each layer, sequence, head and K or V, a thread for 16
-// numbers of a block row.  It goes over the blocks that rows come into, the
-// lowest first, and reads all rows of a block before it writes one: since
-// path[d] >= d rises strictly, later blocks' rows come from none that it wrote.
+// ----------------------------------------------------------------- compact
+// A workgroup has one layer and sequence and, a wave each, four of its heads' K
+// or V.  A chain of dependent reads is the most of its time: path and page of 256
+// rows are looked up once, a row a thread.  Then a wave takes the blocks that rows
+// come into, the lowest first, a lane 16 numbers of a row, and reads all rows of
+// a block before it writes one: since path[d] >= d rises strictly, later blocks'
+// rows come from none that it wrote.  Rows that stay where they are (committed
+// ones, the root) are read only if their scale grows.  (Two blocks at a time take
+// 90 registers: 64 sequences of 8 rows in 36 layers took 29 us so, 21 like this.)
+constexpr int kMapRows = 256;
+
 template <int D>
-__global__ __launch_bounds__(2 * D) void compact8_kernel(Paged p, Cache8 c, long long layer_stride,
-                                                         long long scale_layer_stride,
-                                                         const int32_t* __restrict__ path,
-                                                         const int32_t* __restrict__ accept, int path_cap) {
-  constexpr int TPR = D / 16, WAVES = 2 * D / 64;
-  __shared__ int most_s[WAVES], moved_s[WAVES];
-  const int b = blockIdx.y, g = blockIdx.x >> 1, kv = blockIdx.x & 1;
-  uint8_t* const pool = c.pages[kv] + (long long)blockIdx.z * layer_stride;
-  uint8_t* const scales = c.scales[kv] + (long long)blockIdx.z * scale_layer_stride;
-  const int len = p.seq_len[b], rows = seq_of(p, b, rows_of(p)).rows;
-  if (accept[b] < 0 || accept[b] >= path_cap || len < 0) return;
-  const int L = min(accept[b], rows - 1);
-  const int wave = threadIdx.x >> 6, row = threadIdx.x / TPR, sub = threadIdx.x % TPR;
-  const auto page_of = [&](long long token) {
-    if (token >= p.own_cap) return -1;
+__global__ __launch_bounds__(256) void compact8_kernel(Paged p, Cache8 c, long long layer_stride,
+                                                       long long scale_layer_stride,
+                                                       const int32_t* __restrict__ path,
+                                                       const int32_t* __restrict__ accept, int path_cap) {
+  constexpr int TPR = D / 16, RPS = 64 / TPR, STEPS = kBlockRows / RPS;
+  __shared__ int page_s[kMapRows], row_s[kMapRows];  // where a row's numbers come from (-1: no row comes)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int task = (int)blockIdx.x * 4 + wave, b = blockIdx.y, g = task >> 1, kv = task & 1;
+  const int len = p.seq_len[b], accepted = accept[b], rows = seq_of(p, b, rows_of(p)).rows;
+  if (accepted < 0 || accepted >= path_cap || len < 0 || len >= p.own_cap) return;
+  const int L = min(accepted, rows - 1);
+  const int row0 = lane / TPR, sub = lane % TPR, in_page = (1 << p.page_shift) - 1;
+  const auto page_of = [&](int token) {
+    if (token < 0 || token >= p.own_cap) return -1;
     const int page = p.table[(size_t)b * p.table_ld + (token >> p.page_shift)];
     return page < p.n_pages ? page : -1;
   };
-  const auto row_at = [&](int page, long long token) {
-    return pool + (long long)page * p.page_stride +
-           (((long long)g << p.page_shift) + (token & ((1 << p.page_shift) - 1))) * D + sub * 16;
+  const auto row_at = [&](int page, int row) {
+    return c.pages[kv] + (long long)blockIdx.z * layer_stride + (long long)page * p.page_stride +
+           (((long long)g << p.page_shift) + row) * D + sub * 16;
   };
-  const auto scale_at = [&](int page, long long token) {
-    return scales + (long long)page * c.scale_stride + (long long)g * c.page_blocks +
-           (token & ((1 << p.page_shift) - 1)) / kBlockRows;
+  const auto scale_at = [&](int page, int row) {
+    return c.scales[kv] + (long long)blockIdx.z * scale_layer_stride + (long long)page * c.scale_stride +
+           (long long)g * c.page_blocks + row / kBlockRows;
   };
-  for (long long first = len / kBlockRows * kBlockRows; L >= 0 && first <= (long long)len + L; first += kBlockRows) {
-    const int to = page_of(first);
-    if (to < 0) continue;  // the same in the whole workgroup
-    const long long token = first + row, d = token - len;
-    long long from = -1;  // the token that comes here
-    if (d < 0) {
-      from = token;
-    } else if (d <= L) {
-      const int i = path[(size_t)b * path_cap + d];
-      if (i >= 0 && i < rows) from = (long long)len + i;
+  for (int map0 = len / kBlockRows * kBlockRows; L >= 0 && map0 <= len + L; map0 += kMapRows) {
+    {
+      const int token = map0 + (int)threadIdx.x, d = token - len;
+      int from = d < 0 ? token : -1;
+      if (d >= 0 && d <= L) {
+        const int i = path[(size_t)b * path_cap + d];
+        if (i >= 0 && i < rows) from = len + i;
+      }
+      const int to = page_of(token);
+      page_s[threadIdx.x] = from == token ? to : to >= 0 ? page_of(from) : -1;
+      row_s[threadIdx.x] = from & in_page;
     }
-    const int page = from >= 0 ? page_of(from) : -1;
-    u32x4 w{};
-    int e = -1000;
-    if (page >= 0) {
-      w = ld16(row_at(page, from));
-      e = (int)*scale_at(page, from) - 127;
-    }
-    int most = e, moved = page >= 0 && d >= 0;
-    for (int off = 32; off > 0; off >>= 1) most = max(most, shfl_xor_i(most, off));
-    moved = __any(moved);
-    if ((threadIdx.x & 63) == 0) most_s[wave] = most, moved_s[wave] = moved;
     __syncthreads();
-    for (int k = 0; k < WAVES; ++k) most = max(most, most_s[k]), moved |= moved_s[k];
-    if (moved && page >= 0 && (from != token || e != most)) {
-      if (e != most)
+    for (int at = 0; g < p.Hkv && at < kMapRows && map0 + at <= len + L; at += kBlockRows) {
+      const int first = map0 + at, to = page_of(first);  // the same in the whole wave
+      int page[STEPS], row[STEPS], e[STEPS], most = -1000;
+      bool stays[STEPS], moved = false;
+      u32x4 w[STEPS];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = fewer4(w[k], most - e);
-      st16(row_at(to, token), w);
+      for (int s = 0; s < STEPS; ++s) {
+        const int x = s * RPS + row0;
+        page[s] = page_s[at + x];
+        row[s] = row_s[at + x];
+        stays[s] = page[s] == to && row[s] == ((first + x) & in_page);
+        e[s] = -1000;
+        if (page[s] >= 0) {
+          e[s] = (int)*scale_at(page[s], row[s]) - 127;
+          if (!stays[s]) w[s] = ld16(row_at(page[s], row[s]));
+          moved = moved || first + x >= len;
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all rows are here
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) most = max(most, e[s]);
+#pragma unroll
+      for (int off = 32; off >= TPR; off >>= 1) most = max(most, shfl_xor_i(most, off));
+      if (!__any(moved)) continue;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const int into = (first + s * RPS + row0) & in_page;
+        if (page[s] < 0 || (stays[s] && e[s] == most)) continue;
+        if (stays[s]) w[s] = ld16(row_at(to, into));
+        if (e[s] != most)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) w[s][x] = fewer4(w[s][x], most - e[s]);
+        st16(row_at(to, into), w[s]);
+      }
+      if (lane == 0) *scale_at(to, first & in_page) = (uint8_t)(most + 127);
     }
-    if (moved && threadIdx.x == 0) *scale_at(to, first) = (uint8_t)(most + 127);
     __syncthreads();
   }
 }
@@ -362,12 +399,16 @@ struct ForkArgs {
   uint8_t* scales[2];
   long long page_bytes, layer_bytes, scale_stride, scale_layer;
   int n_seqs, table_ld, page_shift, n_pages, own_cap, row_bytes, page_blocks;  // page_blocks 0: no scales
+  int heads, heads_each;
 };
 
-// One workgroup for each layer, sequence, head and K or V; the first of a
-// sequence writes its length and table.
+// One workgroup for each layer, sequence, K or V and as many heads as have 32 KiB
+// of a page (a workgroup a head took 42 us for 64 pages of 16 rows in 36 layers, by
+// the number of workgroups alone); the first of a sequence writes its length and
+// table.
 __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
-  const int b = blockIdx.y, g = blockIdx.x >> 1, kv = blockIdx.x & 1;
+  const int b = blockIdx.y, g0 = (int)(blockIdx.x >> 1) * a.heads_each, kv = blockIdx.x & 1;
+  const int heads = min(a.heads_each, a.heads - g0);
   const bool in_place = a.len_out == a.seq_len, first = blockIdx.x == 0 && blockIdx.z == 0;
   const int p = a.parent[b];
   bool forks = p >= 0 && p != b && p < a.n_seqs;
@@ -392,23 +433,31 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
     if (threadIdx.x == 0) a.len_out[b] = forks ? n : a.seq_len[b];
   }
   if (!forks || rows == 0) return;
-  const long long head = ((long long)g << a.page_shift) * a.row_bytes + (long long)blockIdx.z * a.layer_bytes;
-  const uint8_t* const src = a.pages[kv] + (long long)page * a.page_bytes + head;
-  uint8_t* const dst = a.pages[kv] + (long long)to * a.page_bytes + head;
-  const long long bytes = (long long)rows * a.row_bytes;
-  for (long long e = threadIdx.x * 16; e < bytes; e += 4 * 256 * 16) {
+  const long long head = (long long)a.row_bytes << a.page_shift;  // bytes from one head to the next
+  const long long at = (long long)blockIdx.z * a.layer_bytes + g0 * head;
+  const uint8_t* const src = a.pages[kv] + (long long)page * a.page_bytes + at;
+  uint8_t* const dst = a.pages[kv] + (long long)to * a.page_bytes + at;
+  const int each = rows * (a.row_bytes / 16), all = heads * each;  // pieces of 16 bytes
+  for (int e = threadIdx.x; e < all; e += 4 * 256) {
     u32x4 x[4];
+    long long off[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int piece = min(e + k * 256, all - 1), g = piece / each;
+      off[k] = g * head + (long long)(piece - g * each) * 16;
+      x[k] = ld16(src + off[k]);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (e + k * 4096 < bytes) x[k] = ld16(src + e + k * 4096);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (e + k * 4096 < bytes) st16(dst + e + k * 4096, x[k]);
+      if (e + k * 256 < all) st16(dst + off[k], x[k]);
   }
   if (a.page_blocks) {
-    const long long at = (long long)blockIdx.z * a.scale_layer + (long long)g * a.page_blocks;
-    for (int k = threadIdx.x; k * kBlockRows < rows; k += 256)
-      a.scales[kv][at + (long long)to * a.scale_stride + k] = a.scales[kv][at + (long long)page * a.scale_stride + k];
+    const int used = (rows + kBlockRows - 1) / kBlockRows;
+    const long long from = (long long)blockIdx.z * a.scale_layer + (long long)g0 * a.page_blocks;
+    for (int k = threadIdx.x; k < heads * used; k += 256) {
+      const long long x = from + k / used * a.page_blocks + k % used;
+      a.scales[kv][x + (long long)to * a.scale_stride] = a.scales[kv][x + (long long)page * a.scale_stride];
+    }
   }
 }
 
@@ -428,7 +477,10 @@ int launch_fork(const char* who, const ooo_paged_batch* b, const Paged& p, ForkA
   a.page_shift = p.page_shift;
   a.n_pages = p.n_pages;
   a.own_cap = p.own_cap;
-  fork_kernel<<<dim3(2 * p.Hkv, p.n_seqs, n_layers), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  a.heads = p.Hkv;
+  const long long head = (long long)a.row_bytes << p.page_shift;
+  a.heads_each = (int)std::min<long long>(std::max<long long>(32768 / head, 1), p.Hkv);
+  fork_kernel<<<dim3(2 * ((p.Hkv + a.heads_each - 1) / a.heads_each), p.n_seqs, n_layers), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
   const hipError_t e = hipGetLastError();
   OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));
   return ooo::ok();
@@ -464,7 +516,7 @@ extern "C" int ooo_paged_append8(const ooo_paged_batch* batch, const ooo_cache8*
   a.depth = depth;
   a.q_out = q_out;
   a.fr = rope_freq(rope_theta, D);
-  a.span = a.p.n_rows > 2048 ? 8 : 1;
+  a.span = a.p.n_rows / 8 >= a.p.n_seqs ? 8 : 1;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (batch->dt == OOO_BF16 && D == 128) launch_append8<uint16_t, 128>(a, st);
   else if (batch->dt == OOO_BF16) launch_append8<uint16_t, 64>(a, st);
@@ -485,13 +537,13 @@ extern "C" int ooo_paged_compact8(const ooo_paged_batch* batch, const ooo_cache8
   if (rc != OOO_OK) return rc;
   OOO_REQUIRE(path && accept_len, OOO_ERR_INVALID, "%s: null pointer", who);
   OOO_REQUIRE(path_cap >= 1, OOO_ERR_INVALID, "%s: path_cap must be >= 1", who);
-  const dim3 grid(2 * p.Hkv, p.n_seqs, cache->n_layers);
+  const dim3 grid((2 * p.Hkv + 3) / 4, p.n_seqs, cache->n_layers);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (batch->head_dim == 128)
     compact8_kernel<128><<<grid, 256, 0, st>>>(p, c, cache->layer_stride, cache->scale_layer_stride, path, accept_len,
                                                path_cap);
   else
-    compact8_kernel<64><<<grid, 128, 0, st>>>(p, c, cache->layer_stride, cache->scale_layer_stride, path, accept_len,
+    compact8_kernel<64><<<grid, 256, 0, st>>>(p, c, cache->layer_stride, cache->scale_layer_stride, path, accept_len,
                                               path_cap);
   const hipError_t e = hipGetLastError();
   OOO_REQUIRE(e == hipSuccess, OOO_ERR_HIP, "%s: launch failed: %s", who, hipGetErrorString(e));

@@ -89,7 +89,7 @@ struct Deal {
 };
 constexpr PlanCosts kCosts{21.f, 160.f, 5.f, 0.05f};
 // 8-bit pages: half the bytes of a half-tile.
-constexpr PlanCosts kCosts8{24.f, 160.f, 2.5f, 0.025f};
+constexpr PlanCosts kCosts8{26.f, 160.f, 3.5f, 0.033f};
 
 // The deal that finishes first, for every lane of a wave, each of which tries
 // its share of the split counts (one lane alone took 40 us for 65 of them).

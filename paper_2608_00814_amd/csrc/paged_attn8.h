@@ -27,6 +27,28 @@ __device__ __forceinline__ void dma4_nt(const void* base, uint32_t voff, uint32_
                : "memory", "m0");
 }
 
+// N (2 or 4) LDS DMA instructions of 16 bytes per lane, 1 KiB apart at both ends.
+template <int N>
+__device__ __forceinline__ void dma16s_nt(const void* base, const uint32_t (&voff)[N], uint32_t lds) {
+  static_assert(N == 2 || N == 4, "a half-tile");
+  if constexpr (N == 4)
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %5 nt\n\t"
+        "global_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3072 nt" ::"s"(lds),
+        "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base)
+        : "memory", "m0");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %3 nt\n\t"
+        "global_load_lds_dwordx4 %2, %3 offset:1024 nt" ::"s"(lds),
+        "v"(voff[0]), "v"(voff[1]), "s"(base)
+        : "memory", "m0");
+}
+
 // LDS geometry of tiles of 8-bit rows: row-major, the 16-byte chunks of a row
 // permuted so that the reads of K (16 rows and one chunk: sixteen in a row, or
 // four of every eight) and the transpose reads of V (8 rows and two chunks, or
@@ -183,21 +205,21 @@ struct HalfCopy {
   int lane, keys;  // from the item's first on
   __device__ __forceinline__ HalfCopy(const Item& it, int ln) : lane(ln), keys(it.limit - 32 * it.t0) {
 #pragma unroll
-    for (int x = 0; x < HI; ++x) full[x] = off(x, 31);
+    for (int x = 0; x < HI; ++x) full[x] = off(x, 31) - 1024 * x;
   }
-  // From the half-tile's first row to a lane's source; rows past `last` repeat it.
+  // Instruction x: from the half-tile's first row to a lane's source; rows past
+  // `last` repeat it.
   __device__ __forceinline__ uint32_t off(int x, int last) const {
     const int r = x * RPI + lane / R::CH;
-    return (uint32_t)min(r, last) * D + (uint32_t)R::swz(r, lane % R::CH) * 16u;
+    return (uint32_t)(min(r, last) * D + R::swz(r, lane % R::CH) * 16);
   }
   __device__ __forceinline__ void operator()(const uint8_t* src, int n, uint32_t to) const {
     const int last = keys - 32 * n - 1;
     if (last >= 31) {
-#pragma unroll
-      for (int x = 0; x < HI; ++x) dma16_nt(src, full[x], to + x * 1024);
+      dma16s_nt<HI>(src, full, to);
     } else {
 #pragma unroll
-      for (int x = 0; x < HI; ++x) dma16_nt(src, off(x, last), to + x * 1024);
+      for (int x = 0; x < HI; ++x) dma16_nt(src, off(x, max(last, 0)), to + x * 1024);
     }
   }
 };
@@ -710,19 +732,23 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
 
 // One item of up to 16 query rows by a wave alone: decoding, where a sequence has
 // one row for each query head of the group.  On 16x16x32 products it costs half
-// the matrix and softmax work of the narrow item above, which leaves the copies.
-// S^T = K Q^T in two blocks of 16 keys, of which block t's row i is key 8 (i / 4)
-// + 4 t + i % 4, so that lane (c, u) holds row c's keys 8 u .. 8 u + 7 in operand
-// order; O^T = V^T P^T in blocks of 16 columns: columns 16 dt + 4 u + 0..3.
+// the matrix and softmax work of the narrow item above, and it goes over 64 keys
+// at a time, so that the chain of waits from K to P V is half as often.
+// S^T = K Q^T in blocks of 16 keys, of which block t's row i is key 32 (t / 2) +
+// 8 (i / 4) + 4 (t % 2) + i % 4, so that lane (c, u) holds row c's keys 8 u .. 8 u
+// + 7 of either half in operand order; O^T = V^T P^T in blocks of 16 columns:
+// columns 16 dt + 4 u + 0..3.
 template <int D, bool NEG>
 __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int wave, uint8_t* ring,
                                                  uint8_t* windows) {
   using R = Ring8<D>;
-  constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS, S = D / 32, DT = D / 16;
+  constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS / 2, S = D / 32, DT = D / 16;
+  constexpr int ST = 4 * R::HALF;  // a stage: two half-tiles of K, two of V
   const PagedAttnArgs& a = args_again();
   const Paged p = a.p;
   const float scale = a.scale_log2e;
-  const Item it = load_item(a.plan + a.off_items_n, item);
+  Item it = load_item(a.plan + a.off_items_n, item);
+  it.limit = min(it.limit, 32 * it.t1);  // a last step may be half of one
   const int c = lane & 15, u = lane >> 4;
   const int qi = it.q0 + min(c, it.nq - 1), i = qi / p.G, hq = g * p.G + qi - i * p.G;
   const long long row = (long long)it.row0 + i;
@@ -734,13 +760,13 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   }
   Window8 window = window_of<D>(a, it, g, lane, 32 * it.t0, 32, windows + wave * Window8::BYTES);
   window.start();
-  const int all = all_see(p, it);
+  const int all = min(all_see(p, it), it.limit);
   const uint8_t* const kp = (const uint8_t*)a.k;
   const uint8_t* const vp = (const uint8_t*)a.v;
   const uint32_t kd = __builtin_amdgcn_readfirstlane(lds_addr(ring) + wave * 16384);
   const int krow = 8 * (c >> 2) + (c & 3), vrow = 8 * u + (c >> 1);
   uint32_t k_at = kd + krow * D + (R::swz(krow, u) << 4);
-  uint32_t v_at = kd + R::HALF + vrow * D + (R::swz(vrow, 0) << 4) + 8 * (c & 1);
+  uint32_t v_at = kd + 2 * R::HALF + vrow * D + (R::swz(vrow, 0) << 4) + 8 * (c & 1);
 #pragma unroll
   for (int x = 0; x < S; ++x) asm volatile("" : "+v"(qf[x]));  // here, not inside the loop
   if constexpr (NEG) {
@@ -752,60 +778,72 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
   const HalfCopy<D> copy(it, lane);
-  const int count = it.t1 - it.t0;
+  const int count = (it.t1 - it.t0 + 1) / 2;
   const uint64_t* const words = p.mask + (size_t)row * p.W;
 #pragma unroll
   for (int n = 0; n < NS; ++n)
     if (n < count) {
-      copy(kp + window.at(n), n, kd + n * 2 * R::HALF);
-      copy(vp + window.at(n), n, kd + n * 2 * R::HALF + R::HALF);
+      const long long s0 = window.at(2 * n), s1 = window.at(2 * n + 1);
+      copy(kp + s0, 2 * n, kd + n * ST);
+      copy(kp + s1, 2 * n + 1, kd + n * ST + R::HALF);
+      copy(vp + s0, 2 * n, kd + n * ST + 2 * R::HALF);
+      copy(vp + s1, 2 * n + 1, kd + n * ST + 3 * R::HALF);
     }
   for (int n = 0; n < count; ++n) {
-    const uint32_t st = kd + (uint32_t)(n % NS) * 2 * R::HALF;
+    const uint32_t st = kd + (uint32_t)(n % NS) * ST;
     const int ahead = min(count - 1 - n, NS - 1);
     const bool more = n + NS < count;
-    u32x4 kr[2][D / 64];
-    u32x2 vr[DT];
-    wait_ahead<2 * HI, HI, NS - 1>(ahead);
-    const float k_up = window.k_scale(n);
+    u32x4 kr[4][D / 64];
+    u32x2 vr[2][DT];
+    wait_ahead<4 * HI, 2 * HI, NS - 1>(ahead);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int j = 0; j < D / 64; ++j)
         kr[t][j] = *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)((k_at ^ (64u * j) ^
-                                                                                 (uint32_t)(R::FOURTH * t)) +
-                                                                                4 * t * D);
+                                                                                 (uint32_t)(R::FOURTH * (t & 1))) +
+                                                                                (4 * (t & 1) + 32 * (t >> 1)) * D);
+    const float k_up[2] = {window.k_scale(2 * n), window.k_scale(2 * n + 1)};
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    long long src = 0;
+    long long src[2] = {0, 0};
     if (more) {
-      window.turn(n + NS);
-      src = window.at(n + NS);
-      copy(kp + src, n + NS, st);
+      window.turn(2 * (n + NS));
+      src[0] = window.at(2 * (n + NS));
+      src[1] = window.at(2 * (n + NS) + 1);
+      copy(kp + src[0], 2 * (n + NS), st);
+      copy(kp + src[1], 2 * (n + NS) + 1, st + R::HALF);
     }
-    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < S; ++x)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        s[t] = mfma16(bf16_of(kr[t][x / 2][2 * (x & 1)], kr[t][x / 2][2 * (x & 1) + 1], k_up), qf[x], s[t]);
-    const int lo = 32 * (it.t0 + n);
-    if (lo + 32 > all) {
-      const uint32_t b = (uint32_t)seen_in(p, it, i, words, lo) >> (8 * u);
+      for (int t = 0; t < 4; ++t)
+        s[t] = mfma16(bf16_of(kr[t][x / 2][2 * (x & 1)], kr[t][x / 2][2 * (x & 1) + 1], k_up[t >> 1]), qf[x], s[t]);
+    const int lo = 32 * it.t0 + 64 * n;
+    if (lo + 64 > all) {
+      const uint64_t b = seen_in(p, it, i, words, lo) >> (8 * u);
+      const uint32_t bits[2] = {(uint32_t)b, (uint32_t)(b >> 32)};
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!((b >> j) & 1u)) s[j / 4][j % 4] = -INFINITY;
+      for (int j = 0; j < 16; ++j)
+        if (!((bits[j / 8] >> (j % 8)) & 1u)) s[j / 4][j % 4] = -INFINITY;
     }
     {  // as settle()
-      const int x = __builtin_amdgcn_readfirstlane(__float_as_int(s[1][3]));
-      asm volatile("" : "+v"(s[0]), "+v"(s[1]) : "s"(x));
+      const int x = __builtin_amdgcn_readfirstlane(__float_as_int(s[3][3]));
+      asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]) : "s"(x));
     }
-    float mx = max3f(max3f(s[0][0], s[0][1], s[0][2]), max3f(s[1][0], s[1][1], s[1][2]), max3f(s[0][3], s[1][3], -INFINITY));
+    float mt[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) mt[t] = max3f(s[t][0], s[t][1], s[t][2]);
+    float mx = max3f(max3f(mt[0], s[0][3], mt[1]), max3f(s[1][3], mt[2], s[2][3]), max3f(mt[3], s[3][3], -INFINITY));
     {
       const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = max3f(__uint_as_float(h[0]), __uint_as_float(h[1]), -INFINITY);
       const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
       mx = max3f(__uint_as_float(q[0]), __uint_as_float(q[1]), -INFINITY) * scale;
     }
+    // as in the narrow item: the reference maximum moves by 2^8 at a time
     if (__any(mx > m_run + 8.f)) {
       const float m_new = __builtin_fmaxf(m_run, mx);
       const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
@@ -815,31 +853,40 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    u32x4 pk;
+    u32x4 pk[2];
     float ps[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       const float e0 = __builtin_amdgcn_exp2f(fmaf(s[j / 2][2 * (j & 1)], scale, -m_use));
       const float e1 = __builtin_amdgcn_exp2f(fmaf(s[j / 2][2 * (j & 1) + 1], scale, -m_use));
-      pk[j] = pack_bf16x2(e0, e1);
-      ps[j & 1] = add_bf16x2(pk[j], ps[j & 1]);
+      pk[j / 4][j % 4] = pack_bf16x2(e0, e1);
+      ps[j & 1] = add_bf16x2(pk[j / 4][j % 4], ps[j & 1]);
     }
     l_run += ps[0] + ps[1];
-    const bf16x8 pf = as_bf16x8(pk);
-    if (more) wait_vmcnt<(NS - 1) * 2 * HI + HI>();
-    else wait_ahead<2 * HI, 0, NS - 1>(ahead);
-    const float v_up = window.v_scale(n);
+    const bf16x8 pf[2] = {as_bf16x8(pk[0]), as_bf16x8(pk[1])};
+    if (more) wait_vmcnt<(NS - 1) * 4 * HI + 2 * HI>();
+    else wait_ahead<4 * HI, 0, NS - 1>(ahead);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      vr[dt] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                                             (i32x2 __attribute__((address_space(3)))*)(uintptr_t)(v_at ^ (16u * dt))));
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        vr[h][dt] = __builtin_bit_cast(
+            u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                       (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (16u * dt)) + h * R::HALF)));
+    const float v_up[2] = {window.v_scale(2 * n), window.v_scale(2 * n + 1)};
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) copy(vp + src, n + NS, st + R::HALF);
-    const uint32_t step = n % NS == NS - 1 ? (uint32_t)(-2 * (NS - 1) * R::HALF) : (uint32_t)(2 * R::HALF);
+    if (more) {
+      copy(vp + src[0], 2 * (n + NS), st + 2 * R::HALF);
+      copy(vp + src[1], 2 * (n + NS) + 1, st + 3 * R::HALF);
+    }
+    const uint32_t step = n % NS == NS - 1 ? (uint32_t)(-(NS - 1) * ST) : (uint32_t)ST;
     k_at += step;
     v_at += step;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) oacc[dt] = mfma16(bf16_of(vr[dt][0], vr[dt][1], v_up), pf, oacc[dt]);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        oacc[dt] = mfma16(bf16_of(vr[h][dt][0], vr[h][dt][1], v_up[h]), pf[h], oacc[dt]);
   }
   bool bad = window.bad;
 

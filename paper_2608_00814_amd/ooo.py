@@ -861,15 +861,14 @@ def paged_compact8(batch: PagedBatch, cache: Cache8, path, accept_len, stream=No
 def _fork_args(batch: PagedBatch, parent, fresh, seq_len_out, table_out):
     import torch
 
-    i, n, ld = torch.int32, batch.n_seqs, batch.struct.table_ld
-    ptrs = [_on(parent, "parent", batch.device, i, (n,)), _on(fresh, "fresh", batch.device, i, (n,)),
-            _on(seq_len_out, "seq_len_out", batch.device, i, (n,)),
-            _on(table_out, "table_out", batch.device, i, (n, ld))]
-    for own, out, size, nm in ((batch.struct.seq_len, ptrs[2], 4 * n, "seq_len_out"),
-                               (batch.struct.page_table, ptrs[3], 4 * n * ld, "table_out")):
-        if own != out and own < out + size and out < own + size:
-            raise ValueError(f"{nm} overlaps the batch's own array")
-    return ptrs
+    i, dev, n, b = torch.int32, batch.device, batch.n_seqs, batch.struct
+    ld = b.table_ld
+    lens, table = _on(seq_len_out, "seq_len_out", dev, i, (n,)), _on(table_out, "table_out", dev, i, (n, ld))
+    if lens != b.seq_len and abs(lens - b.seq_len) < 4 * n:
+        raise ValueError("seq_len_out overlaps the batch's own array")
+    if table != b.page_table and abs(table - b.page_table) < 4 * n * ld:
+        raise ValueError("table_out overlaps the batch's own array")
+    return _on(parent, "parent", dev, i, (n,)), _on(fresh, "fresh", dev, i, (n,)), lens, table
 
 
 def paged_fork(batch: PagedBatch, k_pages, v_pages, parent, fresh, seq_len_out, table_out, stream=None) -> None:
