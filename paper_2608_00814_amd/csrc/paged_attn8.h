@@ -487,6 +487,12 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
       barrier(1);
       k_at += to_next(0);
       kread(kr);
+      bf16x8 kf[S];
+      {
+        const float up = window.k_scale(min(1, tiles - 1));
+#pragma unroll
+        for (int x = 0; x < S; ++x) kf[x] = bf16_of(kr[x / 2][2 * (x & 1)], kr[x / 2][2 * (x & 1) + 1], up);
+      }
       if (kh0 == 1) ask_v(2, 1);
       ask_k(4);
       auto tile = [&](auto plain, int n) OOO_INLINE {
@@ -500,9 +506,9 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
             barrier(n + 2);
           }
         };
-        const float k_up = window.k_scale(n + 1 < tiles ? n + 1 : n), v_up = window.v_scale(n);
+        const float k_up = window.k_scale(min(n + 2, tiles - 1)), v_up = window.v_scale(n);
         if (kh0 == 1) turn();
-        f32x16 next = score1(0, kr, k_up, f32x16{});
+        f32x16 next = mfma32(kf[0], qf[0], f32x16{});
         const int nv = n + 2 + kh0;
         const uint8_t* const v_src = vp + (kh0 == 0 ? src[2] : src[1]);
         const uint32_t v_to = dst + V0 + stage(nv);
@@ -513,11 +519,11 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
         settle(sc);
         const float m_use = new_max(row_max(sc, [&]() OOO_INLINE {
           __builtin_amdgcn_sched_barrier(0);
-          next = score1(1, kr, k_up, next);
+          next = mfma32(kf[1], qf[1], next);
           __builtin_amdgcn_sched_barrier(0);
         }));
         weights(sc, m_use, pf, [&](int k) OOO_INLINE {
-          if (k + 2 < S) next = score1(k + 2, kr, k_up, next);
+          if (k + 2 < S) next = mfma32(kf[k + 2], qf[k + 2], next);
           if (k < S) vr[k] = vread(k);
           if (PLAIN && k == 2) copy_full(v_src, v_to, 0);
           if (PLAIN && k == 5) copy_full(v_src, v_to, 1);
@@ -534,11 +540,16 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
 #pragma unroll
         for (int x = 0; x < S; ++x) {
           pv(x, vr[x], v_up, pf);
+          // K of tile n + 2: a read for two fragments, which follow two products later
           if (x % 2 == 0) kr[x / 2] = kread1(x / 2);
+          if (x >= 2) kf[x - 2] = bf16_of(kr[x / 2 - 1][2 * (x & 1)], kr[x / 2 - 1][2 * (x & 1) + 1], k_up);
           if (PLAIN && x == S / 4) copy_full(kp + src[0], k_to, 0);
           if (PLAIN && x == S - S / 4) copy_full(kp + src[0], k_to, 1);
           __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int x = S - 2; x < S; ++x)
+          kf[x] = bf16_of(kr[x / 2][2 * (x & 1)], kr[x / 2][2 * (x & 1) + 1], k_up);
         sc = next;
       };
       for (int n = 0; n < tiles; ++n) {

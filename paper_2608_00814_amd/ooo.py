@@ -558,6 +558,9 @@ def swiglu(gate_up, out, n_rows: Optional[int] = None, stream=None) -> None:
 
 def _on(t, name: str, device, dtype=None, shape=None):
     """``t`` as a contiguous tensor of ``device`` (the batch's), or a ValueError."""
+    if ((shape is None or t.shape == shape) and (dtype is None or t.dtype is dtype) and t.is_contiguous()
+            and t.device == device):
+        return t.data_ptr()
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, the batch on {device}")
     if dtype is not None and t.dtype != dtype:
