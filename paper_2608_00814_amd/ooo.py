@@ -618,9 +618,9 @@ class PagedBatch:
         self.dtype = k_pages.dtype if dtype is None and not self.eight else dtype
         if not self.eight and self.dtype != k_pages.dtype:
             raise ValueError(f"dtype must be that of k_pages, {k_pages.dtype}, not {dtype}")
-        if self.dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError(f"dtype must be torch.float32 or torch.bfloat16, not {self.dtype}")
-        b.dt = F32 if self.dtype == torch.float32 else BF16
+        if self.eight and dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+        b.dt = (F32 if dtype == torch.float32 else BF16) if self.eight else dtype_code(k_pages)
         self.device, self.pool = dev, tuple(k_pages.shape)
         self.n_seqs, self.n_rows, self.Hq, self.Hkv, self.D = n, n_rows, n_q_heads, Hkv, D
         b.page_stride = self.page_stride = self._stride_of(k_pages, "k_pages")
