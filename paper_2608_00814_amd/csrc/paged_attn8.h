@@ -50,19 +50,21 @@ __device__ __forceinline__ void dma16s_nt(const void* base, const uint32_t (&vof
 }
 
 // LDS geometry of tiles of 8-bit rows: row-major, the 16-byte chunks of a row
-// permuted so that the reads of K (16 rows and one chunk: sixteen in a row, or
-// four of every eight) and the transpose reads of V (8 rows and two chunks, or
-// 16 rows and one) lie in distinct banks.
+// permuted so that no read meets itself in a bank.  A 16-byte read goes to the
+// banks in groups of lanes 0-3, 12-15 and 20-27, of 4-11, 16-19 and 28-31, and the
+// same 32 on: K's rows are then four quads of rows that differ in bits 2 and 3.
+// The transpose reads of V are of 8 rows and two chunks, or of 16 rows and one.
+// (With bit 4 of the row in the permutation too, every read of K took twice its
+// time, by the count of conflicts.)
 template <int D>
 struct Ring8 {
   static constexpr int CH = D / 16;         // chunks of a row
   static constexpr int MAT = kTile * D;     // bytes of a tile of K or V
   static constexpr int HALF = 32 * D;       // of a half-tile, the rows of one scale
   static constexpr int BYTES = 128 * 1024;  // of the ring: 16 KiB a wave
-  static constexpr int FOURTH = D / 2;      // what four or 16 rows on turn in an address
+  static constexpr int FOURTH = D / 2;      // what four rows on turn in an address
   static __device__ __forceinline__ int swz(int r, int c) {
-    const int x = (r >> 3) & 1, y = ((r >> 2) ^ (r >> 4)) & 1;
-    return c ^ (D == 128 ? x | (r & 2) | y << 2 : x | y << 1);
+    return c ^ (D == 128 ? (r & 6) | ((r >> 3) & 1) : ((r >> 1) & 2) | ((r >> 3) & 1));
   }
 };
 
@@ -263,8 +265,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   // LDS addresses of the fragments in the wave's first stage.  K read j: chunk
   // 2 j + u of row sigma(c), 32 j bytes away by the permutation's exclusive or.
   // V transpose read (16 keys kk, column block dt): row 16 kk + 8 (g16 / 2) +
-  // li / 2, chunk 2 dt + g16 % 2, its half li % 2: 32 dt bytes away, and kk turns
-  // the permutation's bit of row 16.
+  // li / 2, chunk 2 dt + g16 % 2, its half li % 2: 32 dt bytes away.
   const uint32_t k_lds = lds_addr(ring) + (WIDE ? kh0 * R::HALF : wave * 16384);
   const uint32_t v_lds = k_lds + (WIDE ? V0 : R::HALF);
   const int krow = sigma(c), g16 = lane >> 4, li = lane & 15;
@@ -309,8 +310,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   auto vread = [&](int x) OOO_INLINE {  // 16 keys x / DT, column block x % DT
     return __builtin_bit_cast(
         u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                   (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32u * (x % DT)) ^ (uint32_t)(R::FOURTH * (x / DT))) +
-                                                                         16 * (x / DT) * D)));
+                   (i32x2 __attribute__((address_space(3)))*)(uintptr_t)((v_at ^ (32u * (x % DT))) + 16 * (x / DT) * D)));
   };
   auto pv = [&](int x, const u32x2& v, float up, const bf16x8 (&pr)[2]) OOO_INLINE {
     oacc[x % DT] = mfma32(bf16_of(v[0], v[1], up), pr[x / DT], oacc[x % DT]);
@@ -763,11 +763,13 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   const int c = lane & 15, u = lane >> 4;
   const int qi = it.q0 + min(c, it.nq - 1), i = qi / p.G, hq = g * p.G + qi - i * p.G;
   const long long row = (long long)it.row0 + i;
-  bf16x8 qf[S];  // products 2 j and 2 j + 1 take a key's 16 columns 16 (4 j + u) on
+  // products 2 j and 2 j + 1 take a key's 16 columns of chunk `part` + 2 j
+  const int part = R::CH / 2 * (u & 1) + (u >> 1);
+  bf16x8 qf[S];
   {
     const uint16_t* qrow = (const uint16_t*)a.q + (row * p.Hq + hq) * D;
 #pragma unroll
-    for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(ld16(qrow + 16 * (4 * (x / 2) + u) + 8 * (x & 1)));
+    for (int x = 0; x < S; ++x) qf[x] = as_bf16x8(ld16(qrow + 16 * (part + 2 * (x / 2)) + 8 * (x & 1)));
   }
   Window8 window = window_of<D>(a, it, g, lane, 32 * it.t0, 32, windows + wave * Window8::BYTES);
   window.start();
@@ -776,7 +778,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   const uint8_t* const vp = (const uint8_t*)a.v;
   const uint32_t kd = __builtin_amdgcn_readfirstlane(lds_addr(ring) + wave * 16384);
   const int krow = 8 * (c >> 2) + (c & 3), vrow = 8 * u + (c >> 1);
-  uint32_t k_at = kd + krow * D + (R::swz(krow, u) << 4);
+  uint32_t k_at = kd + krow * D + (R::swz(krow, part) << 4);
   uint32_t v_at = kd + 2 * R::HALF + vrow * D + (R::swz(vrow, 0) << 4) + 8 * (c & 1);
 #pragma unroll
   for (int x = 0; x < S; ++x) asm volatile("" : "+v"(qf[x]));  // here, not inside the loop
@@ -811,7 +813,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int j = 0; j < D / 64; ++j)
-        kr[t][j] = *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)((k_at ^ (64u * j) ^
+        kr[t][j] = *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)((k_at ^ (32u * j) ^
                                                                                  (uint32_t)(R::FOURTH * (t & 1))) +
                                                                                 (4 * (t & 1) + 32 * (t >> 1)) * D);
     const float k_up[2] = {window.k_scale(2 * n), window.k_scale(2 * n + 1)};
@@ -935,7 +937,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
         float s = 0.f;
 #pragma unroll
         for (int y = 0; y < D / 64; ++y) {
-          const u32x4 kk = ld16((const uint8_t*)ea.k + base + 16 * (4 * y + u));
+          const u32x4 kk = ld16((const uint8_t*)ea.k + base + 16 * (part + 2 * y));
 #pragma unroll
           for (int h2 = 0; h2 < 2; ++h2) {
             const bf16x8 kb = bf16_of(kk[2 * h2], kk[2 * h2 + 1], ku);

@@ -630,10 +630,10 @@ class PagedBatch:
 
     def _stride_of(self, t, name: str) -> int:
         n_pages, Hkv, rows, D = self.pool
-        page = Hkv * rows * D
-        if tuple(t.shape[-4:]) != self.pool or tuple(t.stride()[-3:]) != (rows * D, D, 1):
+        page, strides = Hkv * rows * D, t.stride()
+        if t.shape[-4:] != self.pool or strides[-3:] != (rows * D, D, 1):
             raise ValueError(f"{name} must be [{n_pages}][{Hkv}][{rows}][{D}] with contiguous pages")
-        s = t.stride(-4) if n_pages > 1 else max(t.stride(-4), page)
+        s = strides[-4] if n_pages > 1 else max(strides[-4], page)
         if s < page:
             raise ValueError(f"{name}: pages overlap")
         return s
