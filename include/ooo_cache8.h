@@ -72,7 +72,8 @@ typedef struct {
  *   others    as for ooo_paged_append
  * Values that are not finite are stored as NaN and ask for no scale; values
  * beyond 448 * 2^119 become that.  A row without a place (ooo_paged_append)
- * gets its q and asks for no scale.
+ * gets its q and asks for no scale.  No two sequences' new rows may lie in one
+ * block (a page that two tables name): its scale and rows would be of either.
  * Errors: as for ooo_paged_append; OOO_ERR_INVALID (layer).
  */
 int ooo_paged_append8(const ooo_paged_batch* batch, const ooo_cache8* cache, int32_t layer, const void* qkv,
@@ -100,7 +101,9 @@ int ooo_paged_attn8(const ooo_paged_batch* batch, const ooo_cache8* cache, int32
  * block that rows come into gets the largest scale of the blocks that these
  * come from, and where it holds committed rows no less than it had; its rows
  * are put under it (rounded to nearest even where they become subnormal).
- * Rows that are not moved by ooo_paged_compact ask for no scale.
+ * Rows that are not moved by ooo_paged_compact ask for no scale.  No two
+ * sequences' new rows may lie in one block (as for ooo_paged_append8).
+ * Errors: as for ooo_paged_compact.
  */
 int ooo_paged_compact8(const ooo_paged_batch* batch, const ooo_cache8* cache, const int32_t* path,
                        const int32_t* accept_len, int32_t path_cap, void* stream);

@@ -18,6 +18,9 @@ namespace {
 // ----------------------------------------------------------------- append
 constexpr int kAppendWaves = 4;
 constexpr int kFewRows = 4096;  // up to so many, a block's heads are shared out
+// Rows of a workgroup of the pages' part where sequences bring several (a block
+// of 32 begins in at most two of them); one row each where most bring one.
+constexpr int kSpan = 8;
 
 // The place of a new row (0 <= r < R: rows_of): its sequence, index in it, own
 // token and page (-1: it has none).
@@ -180,67 +183,63 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int task, int 
     }
   };
   if (m == 1) {
-    {
-      const int groups = (p.Hkv + SLOTS - 1) / SLOTS;
-      const int kv = task >= groups, g0 = (task - kv * groups) * SLOTS, g = g0 + s;
-      Half<T> x;
-      load(x, 0, min(g, p.Hkv - 1), kv);
-      const int was = held ? (int)*scale_at(kv, min(g, p.Hkv - 1)) - 127 : kLeastExp;
-      float lo[N], hi[N];
-      V::unpack(x.a, lo);
-      V::unpack(x.c, hi);
-      if (kv == 0) norm_turn<T, D>(lo, hi, (const T*)a.k_norm, a.eps, j0, cs_s, sn_s);
-      float most = 0.f;
+    const int groups = (p.Hkv + SLOTS - 1) / SLOTS;
+    const int kv = task >= groups, g0 = (task - kv * groups) * SLOTS, g = g0 + s;
+    Half<T> x;
+    load(x, 0, min(g, p.Hkv - 1), kv);
+    const int was = held ? (int)*scale_at(kv, min(g, p.Hkv - 1)) - 127 : kLeastExp;
+    float lo[N], hi[N];
+    V::unpack(x.a, lo);
+    V::unpack(x.c, hi);
+    if (kv == 0) norm_turn<T, D>(lo, hi, (const T*)a.k_norm, a.eps, j0, cs_s, sn_s);
+    float most = 0.f;
 #pragma unroll
-      for (int e = 0; e < N; ++e) most = fmaxf(most, fmaxf(size_of(lo[e]), size_of(hi[e])));
+    for (int e = 0; e < N; ++e) most = fmaxf(most, fmaxf(size_of(lo[e]), size_of(hi[e])));
 #pragma unroll
-      for (int off = LPH / 2; off > 0; off >>= 1) most = fmaxf(most, shfl_xor_f(most, off));
-      const int exp = max(exp_for(most), was);
-      if (g < p.Hkv) {
-        uint8_t* const dst = row_at(kv, g, row) + j0;
-        put_codes<N>(dst, lo, pow2(-exp));
-        put_codes<N>(dst + HALF, hi, pow2(-exp));
-        if (lane % LPH == 0 && (!held || exp != was)) *scale_at(kv, g) = (uint8_t)(exp + 127);
-      }
-      if (held)
-        for (int y = 0; y < min(SLOTS, p.Hkv - g0); ++y) {
-          const int k = __builtin_amdgcn_readlane(exp - was, y * LPH);
-          if (k > 0) regrade(kv, g0 + y, k);
-        }
+    for (int off = LPH / 2; off > 0; off >>= 1) most = fmaxf(most, shfl_xor_f(most, off));
+    const int exp = max(exp_for(most), was);
+    if (g < p.Hkv) {
+      uint8_t* const dst = row_at(kv, g, row) + j0;
+      put_codes<N>(dst, lo, pow2(-exp));
+      put_codes<N>(dst + HALF, hi, pow2(-exp));
+      if (lane % LPH == 0 && (!held || exp != was)) *scale_at(kv, g) = (uint8_t)(exp + 127);
     }
+    if (held)
+      for (int y = 0; y < min(SLOTS, p.Hkv - g0); ++y) {
+        const int k = __builtin_amdgcn_readlane(exp - was, y * LPH);
+        if (k > 0) regrade(kv, g0 + y, k);
+      }
     return;
   }
-  {
-    const int kv = task >= p.Hkv, g = task - kv * p.Hkv;
-    Half<T> x[STEPS];
+  const int kv = task >= p.Hkv, g = task - kv * p.Hkv;
+  Half<T> x[STEPS];
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) load(x[k], min(k * SLOTS + s, m - 1), g, kv);
-    const int was = held ? (int)*scale_at(kv, g) - 127 : kLeastExp;
-    float lo[STEPS][N], hi[STEPS][N], most = 0.f;
+  for (int k = 0; k < STEPS; ++k) load(x[k], min(k * SLOTS + s, m - 1), g, kv);
+  const int was = held ? (int)*scale_at(kv, g) - 127 : kLeastExp;
+  float lo[STEPS][N], hi[STEPS][N], most = 0.f;
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      V::unpack(x[k].a, lo[k]);
-      V::unpack(x[k].c, hi[k]);
-      const int i = min(k * SLOTS + s, m - 1);
-      if (kv == 0) norm_turn<T, D>(lo[k], hi[k], (const T*)a.k_norm, a.eps, j0, cs_s + i * HALF, sn_s + i * HALF);
+  for (int k = 0; k < STEPS; ++k) {
+    V::unpack(x[k].a, lo[k]);
+    V::unpack(x[k].c, hi[k]);
+    const int i = min(k * SLOTS + s, m - 1);
+    if (kv == 0) norm_turn<T, D>(lo[k], hi[k], (const T*)a.k_norm, a.eps, j0, cs_s + i * HALF, sn_s + i * HALF);
 #pragma unroll
-      for (int e = 0; e < N; ++e) most = fmaxf(most, fmaxf(size_of(lo[k][e]), size_of(hi[k][e])));
-    }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, shfl_xor_f(most, off));
-    const int exp = max(exp_for(most), was);
-    const float down = pow2(-exp);
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      const int i = k * SLOTS + s;
-      if (i >= m) continue;
-      uint8_t* const dst = row_at(kv, g, row + i) + j0;
-      put_codes<N>(dst, lo[k], down);
-      put_codes<N>(dst + HALF, hi[k], down);
-    }
-    if (lane == 0 && (!held || exp != was)) *scale_at(kv, g) = (uint8_t)(exp + 127);
-    if (held && exp > was) regrade(kv, g, exp - was);
+    for (int e = 0; e < N; ++e) most = fmaxf(most, fmaxf(size_of(lo[k][e]), size_of(hi[k][e])));
   }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, shfl_xor_f(most, off));
+  const int exp = max(exp_for(most), was);
+  const float down = pow2(-exp);
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k) {
+    const int i = k * SLOTS + s;
+    if (i >= m) continue;
+    uint8_t* const dst = row_at(kv, g, row + i) + j0;
+    put_codes<N>(dst, lo[k], down);
+    put_codes<N>(dst + HALF, hi[k], down);
+  }
+  if (lane == 0 && (!held || exp != was)) *scale_at(kv, g) = (uint8_t)(exp + 127);
+  if (held && exp > was) regrade(kv, g, exp - was);
 }
 
 // Workgroups blockIdx.x < `units` go over the rows from span blockIdx.x on and
@@ -248,7 +247,10 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int task, int 
 // block of its own tokens); the others take four rows of queries each.  Up to
 // kFewRows rows a block's heads go to several workgroups (blockIdx.y), four
 // heads' K or V each: 8 tries of 64 rows took 17.7 us with all heads in one, and
-// take 13.4 so; 10k rows of prompts take 51 with all in one and 59 so.
+// take 13.4 so; 10k rows of prompts take 51 with all in one and 59 so.  11760 rows
+// of prompts, 32 heads of 128 and 8 of K and V, take 63 us (264 MB, 4.2 TB/s of the
+// 4.96 of a copy), the queries' part alone 43 and the pages' alone 33.  A row for
+// each of 256 requests: 5.9 us in a graph.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a, int units) {
   constexpr int HALF = D / 2, SLOTS = 64 / (HALF / Vec16<T>::N);
@@ -290,9 +292,17 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a
   }
 }
 
+struct AppendGrid {
+  long long units, rows;  // workgroups of the pages' part and of the queries'
+};
+AppendGrid append_grid(const AppendArgs& a) {
+  const long long n = a.p.n_rows;
+  return {(n + a.span - 1) / a.span, (n + kAppendWaves - 1) / kAppendWaves};
+}
+
 template <class T, int D>
 void launch_append8(AppendArgs& a, hipStream_t st) {
-  const int units = (a.p.n_rows + a.span - 1) / a.span, rows = (a.p.n_rows + kAppendWaves - 1) / kAppendWaves;
+  const int units = (int)append_grid(a).units, rows = (int)append_grid(a).rows;
   const int tasks = a.p.n_rows > kFewRows ? 1 : (2 * a.p.Hkv + kAppendWaves - 1) / kAppendWaves;
   append8_kernel<T, D><<<dim3(units + rows, tasks), 64 * kAppendWaves, 0, st>>>(a, units);
 }
@@ -516,7 +526,10 @@ extern "C" int ooo_paged_append8(const ooo_paged_batch* batch, const ooo_cache8*
   a.depth = depth;
   a.q_out = q_out;
   a.fr = rope_freq(rope_theta, D);
-  a.span = a.p.n_rows / 8 >= a.p.n_seqs ? 8 : 1;
+  a.span = a.p.n_rows / kSpan >= a.p.n_seqs ? kSpan : 1;
+  const AppendGrid grid = append_grid(a);
+  OOO_REQUIRE((grid.units + grid.rows) * 64 * kAppendWaves < (1ll << 32), OOO_ERR_UNSUPPORTED,
+              "%s: n_rows %d needs more than 2^32 threads", who, a.p.n_rows);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (batch->dt == OOO_BF16 && D == 128) launch_append8<uint16_t, 128>(a, st);
   else if (batch->dt == OOO_BF16) launch_append8<uint16_t, 64>(a, st);

@@ -88,7 +88,10 @@ struct Deal {
   int splits, shared_workers, own_workers, narrow_workers;
 };
 constexpr PlanCosts kCosts{21.f, 160.f, 5.f, 0.05f};
-// 8-bit pages: half the bytes of a half-tile.
+// 8-bit pages: half the bytes of a half-tile, and wide tiles that convert.  256
+// rows over 32k with up to 4k own take 306 us at halves of 3.5 to 4 and shares of
+// HBM of 0.015 to 0.04, and 346 at 2.5, 325 at 4.5 to 7, 328 at a share of 0.05,
+// 690 at a half of 0.5; own keys alone 206 from 0.025 on and 236 at 0.015.
 constexpr PlanCosts kCosts8{26.f, 160.f, 3.5f, 0.033f};
 
 // The deal that finishes first, for every lane of a wave, each of which tries

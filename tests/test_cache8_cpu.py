@@ -95,6 +95,11 @@ def test_append_refusals():
     assert f(qkv=None) == f(q=None) == ooo.ERR_INVALID
     assert f(ld=48 * 128 - 8) == f(eps=-1.0) == f(theta=0.0) == ooo.ERR_INVALID
     assert f(ld=48 * 128 + 4) == f(qkv=P + 2) == f(qn=P + 8) == f(q=P + 8) == ooo.ERR_UNSUPPORTED
+    # more rows than one launch has threads for (rows/8 + rows/4 workgroups of 256)
+    one = dict(n_q_heads=1, n_kv_heads=1, head_dim=64, page_stride=64 * 64)
+    many = batch8(**one, n_rows=(1 << 32) // 96 + 32)
+    assert L.ooo_paged_append8(many, c, 0, P, 3 * 64, None, None, 1e-6, None, 1e6, 2 * P, None) == ooo.ERR_UNSUPPORTED
+    assert b"threads" in L.ooo_last_error()
 
 
 def test_attn_and_plan_refusals():
