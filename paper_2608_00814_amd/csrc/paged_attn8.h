@@ -44,10 +44,10 @@ __device__ __forceinline__ void dma16s_nt(const void* base, const uint32_t (&vof
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
         "global_load_lds_dwordx4 %1, %5 nt\n\t"
-        "global_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\t"
-        "global_load_lds_dwordx4 %4, %5 offset:3072 nt" ::"s"(lds),
-        "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base)
+        "global_load_lds_dwordx4 %2, %5 offset:%6 nt\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:%7 nt\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:%8 nt" ::"s"(lds),
+        "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base), "n"(1024), "n"(2 * 1024), "n"(3 * 1024)
         : "memory", "m0");
   else
     asm volatile(
