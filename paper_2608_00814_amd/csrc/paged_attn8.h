@@ -235,8 +235,9 @@ struct HalfCopy {
   }
 };
 
-// One item by a workgroup (WIDE; every wave calls it) or by a wave alone.
-template <int D, bool NEG, bool WIDE>
+// One item by a workgroup (WIDE; every wave calls it) or by a wave alone.  PAST:
+// its copies go past the caches.
+template <int D, bool NEG, bool WIDE, bool PAST>
 __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int wave, uint8_t* ring,
                                                  uint64_t* mwords, uint8_t* windows, int* bad_s) {
   using R = Ring8<D>;
@@ -417,8 +418,10 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
       }
     };
     auto copy1 = [&](const uint8_t* src, uint32_t off, uint32_t to, int x) OOO_INLINE {
-      if constexpr (D == 128) dma16_nt(src, off, to);
-      else dma4_nt(src, off, to + x * 256);
+      if constexpr (D == 128 && PAST) dma16_nt(src, off, to);
+      else if constexpr (D == 128) dma16(src, off, to);
+      else if constexpr (PAST) dma4_nt(src, off, to + x * 256);
+      else dma4(src, off, to + x * 256);
     };
     uint32_t full_off[PM];
 #pragma unroll
@@ -1003,8 +1006,15 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn
     g = blockIdx.x % a.p.Hkv, worker = blockIdx.x / a.p.Hkv;
     const PlanHead head = load_head(a);
     if (!plan_fits(head, a.want)) return;
+    // Tiles are read by every block of 128 query rows, so their copies keep them in
+    // the caches: 8 tries over 4k 50.6 -> 49.9 us, 512 rows of a prompt over 16k 106
+    // -> 102, 1175 over 4k 99 to 142, by the addresses, -> 89.  Beside many workers
+    // that stream the sequences' own keys they do not: 256 rows over 32k (12 of 32
+    // workers) take 300 us so and 306 else, 128 over 16k with 4 KV heads 84 and 87.
+    const bool past = 4 * head.narrow_workers > (int)gridDim.x / a.p.Hkv;
     each_wide(a, head, worker, [&](int item) OOO_INLINE {
-      paged_attn8_item<D, NEG, true>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+      if (past) paged_attn8_item<D, NEG, true, true>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+      else paged_attn8_item<D, NEG, true, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
     });
   }
   const PagedAttnArgs& a = args_again();
@@ -1018,7 +1028,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn
     if (load_item(a.plan + a.off_items_n, item).nq <= 16)
       paged_attn8_thin<D, NEG>(item, g, lane, wave, ring, windows);
     else
-      paged_attn8_item<D, NEG, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
+      paged_attn8_item<D, NEG, false, true>(item, g, lane, wave, ring, mwords, windows, &bad_s);
   }
 }
 
