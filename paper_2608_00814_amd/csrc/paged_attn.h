@@ -21,7 +21,11 @@ struct PagedAttnArgs {
   float* part_ml;       // [slot][Hkv][group] (m, l)
   long long max_slots;
   float scale_log2e;    // bf16: its size
-  Cache8 c;             // of 8-bit pages
+};
+// The same where pages hold 8-bit numbers.  A struct of its own: in the one above,
+// the cache would change the code of kernels that do not read it.
+struct PagedAttn8Args : PagedAttnArgs {
+  Cache8 c;
 };
 
 // Memory that no kernel writes while it is read here, the same address in the

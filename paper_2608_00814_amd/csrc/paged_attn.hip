@@ -371,7 +371,8 @@ struct Rows32 {
   using Raw = f32x4;
   static __device__ __forceinline__ Raw read(const T* p) { return load4(p); }
   static __device__ __forceinline__ f32x4 get(Raw x, float) { return x; }
-  static __device__ __forceinline__ float scale(const PagedAttnArgs&, int, int, int, int) { return 1.f; }
+  using Args = PagedAttnArgs;
+  static __device__ __forceinline__ float scale(const Args&, int, int, int, int) { return 1.f; }
 };
 struct Rows8 {
   using T = uint8_t;
@@ -382,7 +383,8 @@ struct Rows8 {
     values4(x, up, f);
     return f32x4{f[0], f[1], f[2], f[3]};
   }
-  static __device__ __forceinline__ float scale(const PagedAttnArgs& a, int kv, int page, int g, int row) {
+  using Args = PagedAttn8Args;
+  static __device__ __forceinline__ float scale(const Args& a, int kv, int page, int g, int row) {
     return scale_of(a.c.scales[kv] + (long long)page * a.c.scale_stride + (long long)g * a.c.page_blocks +
                     row / kBlockRows);
   }
@@ -398,7 +400,7 @@ struct Rows8 {
 // dt % 4.  Bound by latency where it is used (float32 is the small option): 53
 // rows of three tries over 128 + 100 tokens take 6.3 us.
 template <int D, class C>
-__global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * kF32Waves, f32_per_cu(D)) void paged_attn_f32_kernel(typename C::Args a) {
   constexpr int NW = kF32Waves;
   constexpr int KS = D / 16;
   __shared__ f32x4 o_s[NW][KS][64];
@@ -698,7 +700,7 @@ __global__ __launch_bounds__(256) void join_kernel(PagedAttnArgs a) {
 }
 
 template <class T, int D>
-void launch_attn(const PagedAttnArgs& a, const PlanShape& s, bool eight, bool neg, hipStream_t st) {
+void launch_attn(const PagedAttn8Args& a, const PlanShape& s, bool eight, bool neg, hipStream_t st) {
   const unsigned items = (unsigned)(s.workers * a.p.Hkv);
   if constexpr (sizeof(T) == 2) {
     if (eight && neg) paged_attn8_kernel<D, true><<<items, 64 * kPagedWaves, 0, st>>>(a);
@@ -740,7 +742,7 @@ int make_plan(const char* who, const ooo_paged_batch* batch, const Paged& p, boo
 }
 
 // a: with the batch, and the cache where it is one of 8 bits.
-int attend(const char* who, const ooo_paged_batch* batch, PagedAttnArgs& a, bool eight, const void* plan,
+int attend(const char* who, const ooo_paged_batch* batch, PagedAttn8Args& a, bool eight, const void* plan,
            size_t plan_bytes, const void* q, const void* k_pages, const void* v_pages, float scale, void* out,
            void* workspace, size_t ws_bytes, void* stream) {
   OOO_REQUIRE(plan && q && k_pages && v_pages && out && workspace, OOO_ERR_INVALID, "%s: null pointer", who);
@@ -820,7 +822,7 @@ extern "C" size_t ooo_paged_attn_workspace(const ooo_paged_batch* batch) {
 extern "C" int ooo_paged_attn(const ooo_paged_batch* batch, const void* plan, size_t plan_bytes, const void* q,
                               const void* k_pages, const void* v_pages, float scale, void* out, void* workspace,
                               size_t ws_bytes, void* stream) {
-  PagedAttnArgs a{};
+  PagedAttn8Args a{};
   const int rc = check_paged("ooo_paged_attn", batch, a.p);
   if (rc != OOO_OK) return rc;
   return attend("ooo_paged_attn", batch, a, false, plan, plan_bytes, q, k_pages, v_pages, scale, out, workspace,
@@ -853,7 +855,7 @@ extern "C" int ooo_paged_attn8(const ooo_paged_batch* batch, const ooo_cache8* c
                                const void* plan, size_t plan_bytes, const void* q, float scale, void* out,
                                void* workspace, size_t ws_bytes, void* stream) {
   const char* const who = "ooo_paged_attn8";
-  PagedAttnArgs a{};
+  PagedAttn8Args a{};
   OOO_REQUIRE(cache, OOO_ERR_INVALID, "%s: cache is null", who);
   int rc = check_cache8(who, batch, cache, a.p, a.c);
   if (rc == OOO_OK) rc = take_layer(who, cache, layer, a.c);

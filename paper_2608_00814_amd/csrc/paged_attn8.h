@@ -180,9 +180,14 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float up) {
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, up, true))});
 }
 
+// As args_again.
+__device__ __forceinline__ const PagedAttn8Args& args8_again() {
+  return static_cast<const PagedAttn8Args&>(args_again());
+}
+
 // The steps of an item, 32 keys each, from key k0 on.
 template <int D>
-__device__ __forceinline__ Window8 window_of(const PagedAttnArgs& a, const Item& it, int g, int lane, int k0, int step,
+__device__ __forceinline__ Window8 window_of(const PagedAttn8Args& a, const Item& it, int g, int lane, int k0, int step,
                                              uint8_t* buf) {
   Window8 w;
   w.ids = it.flags & kShared ? a.p.shared_pages : a.p.table + (size_t)it.seq * a.p.table_ld;
@@ -246,7 +251,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS;
   constexpr int kJoinMl = RG * NP * 64 * 16;  // where the joined halves' statistics lie, behind their sums
   static_assert(8 * R::MAT <= R::BYTES && kJoinMl + RG * 64 * 8 <= R::BYTES, "ring");
-  const PagedAttnArgs& a = args_again();
+  const PagedAttn8Args& a = args8_again();
   const Paged p = a.p;
   const float scale = a.scale_log2e;
   const Item it = load_item(a.plan + (WIDE ? a.off_items_w : a.off_items_n), item);
@@ -627,7 +632,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
   }
   bool bad = window.bad;
 
-  const PagedAttnArgs& ea = args_again();
+  const PagedAttn8Args& ea = args8_again();
   const Paged& ep = ea.p;
   const Item e = load_item(ea.plan + (WIDE ? ea.off_items_w : ea.off_items_n), item);
   const int eq = e.q0 + min(qr, e.nq - 1), ei = eq / ep.G;
@@ -768,7 +773,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   using R = Ring8<D>;
   constexpr int HI = HalfCopy<D>::HI, NS = HalfCopy<D>::NS / 2, S = D / 32, DT = D / 16;
   constexpr int ST = 4 * R::HALF;  // a stage: two half-tiles of K, two of V
-  const PagedAttnArgs& a = args_again();
+  const PagedAttn8Args& a = args8_again();
   const Paged p = a.p;
   const float scale = a.scale_log2e;
   Item it = load_item(a.plan + a.off_items_n, item);
@@ -916,7 +921,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
   }
   bool bad = window.bad;
 
-  const PagedAttnArgs& ea = args_again();
+  const PagedAttn8Args& ea = args8_again();
   const Paged& ep = ea.p;
   const Item e = load_item(ea.plan + ea.off_items_n, item);
   const int eq = e.q0 + min(c, e.nq - 1), ei = eq / ep.G;
@@ -993,7 +998,7 @@ __device__ __forceinline__ void paged_attn8_thin(int item, int g, int lane, int 
 }
 
 template <int D, bool NEG>
-__global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttnArgs) {
+__global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn8Args) {
   __shared__ __attribute__((aligned(1024))) uint8_t ring[Ring8<D>::BYTES];
   __shared__ __attribute__((aligned(1024))) uint64_t mwords[4 * 32 * 16];
   __shared__ __attribute__((aligned(1024))) uint8_t windows[kPagedWaves * Window8::BYTES];
@@ -1002,7 +1007,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int g, worker;
   {
-    const PagedAttnArgs& a = args_again();
+    const PagedAttn8Args& a = args8_again();
     g = blockIdx.x % a.p.Hkv, worker = blockIdx.x / a.p.Hkv;
     const PlanHead head = load_head(a);
     if (!plan_fits(head, a.want)) return;
@@ -1017,7 +1022,7 @@ __global__ __launch_bounds__(64 * kPagedWaves) void paged_attn8_kernel(PagedAttn
       else paged_attn8_item<D, NEG, true, false>(item, g, lane, wave, ring, mwords, windows, &bad_s);
     });
   }
-  const PagedAttnArgs& a = args_again();
+  const PagedAttn8Args& a = args8_again();
   const PlanHead head = load_head(a);
   const int narrow = worker - head.narrow_first;
   if (narrow < 0 || narrow >= head.narrow_workers) return;
