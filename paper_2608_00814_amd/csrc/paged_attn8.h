@@ -571,9 +571,12 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
       };
       for (int n = 0; n < tiles; ++n) {
         // the plain tiles end at the first that some row does not see all of, and
-        // five before one that is not full or begins a window
+        // five before one that is not full or begins a window.  Their wait leaves
+        // two copies on their way, K of tile n + 4 and V of n + 2.  Without that K, V
+        // of n + 1 would be one of them: none in items of less than five tiles (later
+        // runs of them begin behind a copy of that K)
         const int care = min(full, window.base + 64);
-        int end = min(tiles, (all >> 6) - it.t0);
+        int end = tiles < 5 ? 0 : min(tiles, (all >> 6) - it.t0);
         if (care < tiles) end = min(end, care - 5);
 #pragma unroll 1
         for (; n < end; ++n) tile(Yes{}, n);
