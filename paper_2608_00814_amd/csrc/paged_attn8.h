@@ -464,8 +464,8 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
     auto ask_v = [&](int n, int back) OOO_INLINE { copy(vp + src[back], n, dst + V0 + stage(n)); };
     auto barrier = [&](int m) OOO_INLINE {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (m + 2 < tiles) wait_vmcnt<2 * PM>();  // K of m + 2 and V of m may be on their way
-      else if (m < tiles) wait_vmcnt<PM>();
+      if (copies_left(m, tiles) == 2) wait_vmcnt<2 * PM>();
+      else if (copies_left(m, tiles) == 1) wait_vmcnt<PM>();
       else wait_vmcnt<0>();
       wg_barrier();
     };
@@ -570,14 +570,7 @@ __device__ __forceinline__ void paged_attn8_item(int item, int g, int lane, int 
         sc = next;
       };
       for (int n = 0; n < tiles; ++n) {
-        // the plain tiles end at the first that some row does not see all of, and
-        // five before one that is not full or begins a window.  Their wait leaves
-        // two copies on their way, K of tile n + 4 and V of n + 2.  Without that K, V
-        // of n + 1 would be one of them: none in items of less than five tiles (later
-        // runs of them begin behind a copy of that K)
-        const int care = min(full, window.base + 64);
-        int end = tiles < 5 ? 0 : min(tiles, (all >> 6) - it.t0);
-        if (care < tiles) end = min(end, care - 5);
+        const int end = plain_end(tiles, (all >> 6) - it.t0, full, window.base + 64);
 #pragma unroll 1
         for (; n < end; ++n) tile(Yes{}, n);
         if (n < tiles) tile(No{}, n);

@@ -31,6 +31,7 @@
 
 #include "attn_tile.h"
 #include "paged_attn.h"
+#include "wide_schedule.h"
 
 namespace ooo {
 
@@ -334,8 +335,8 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
     auto ask_v = [&](int n, int back) OOO_INLINE { copy(vp + src[back], n, dst + V0 + stage(n)); };
     auto barrier = [&](int m) OOO_INLINE {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (m + 2 < tiles) wait_vmcnt<2 * PM>();  // K of m + 2 and V of m may be on their way
-      else if (m < tiles) wait_vmcnt<PM>();
+      if (copies_left(m, tiles) == 2) wait_vmcnt<2 * PM>();
+      else if (copies_left(m, tiles) == 1) wait_vmcnt<PM>();
       else wait_vmcnt<0>();
       wg_barrier();
     };
@@ -430,15 +431,9 @@ __device__ __forceinline__ void paged_attn_item(int item, int g, int lane, int w
         sc = next;
       };
       for (int n = 0; n < tiles; ++n) {
-        // the plain tiles end at the first that some row does not see all of, and
-        // five before one that is not full or begins a window of pages.  Their wait leaves
-        // two copies on their way, K of tile n + 4 and V of n + 2.  Without that K, V
-        // of n + 1 would be one of them: none in items of less than five tiles (later
-        // runs of them begin behind a copy of that K)
         const int wt = (int)min((long long)tiles,
                                 ((long long)(window.first + window.base + 64) << p.page_shift >> 6) - it.t0);
-        int end = tiles < 5 ? 0 : min(tiles, (all >> 6) - it.t0);
-        if (min(full, wt) < tiles) end = min(end, min(full, wt) - 5);
+        const int end = plain_end(tiles, (all >> 6) - it.t0, full, wt);
 #pragma unroll 1
         for (; n < end; ++n) tile(Yes{}, n);
         if (n < tiles) tile(No{}, n);
