@@ -16,12 +16,16 @@
  * elements are e4m3 numbers (OCP: a sign, four bits of exponent, three of
  * fraction; no infinities), one byte each.  Blocks of 32 consecutive rows of a
  * page share one scale for each KV head, K and V apart: the byte E stands for
- * 2^(E - 127), and an element for its number times that.  A block's scale is
- * the least power of two that brings the values of its rows to at most 448,
- * from 2^-100 to 2^119 (the entry points write no other and read these); it
- * never falls while the block holds committed rows.  A power of two, so that a
- * scale that grows under rows that are there costs them nothing but the last
- * bits of numbers that become subnormal.
+ * 2^(E - 127), and an element for its number times that.  Scales go from 2^-100
+ * to 2^119 (the entry points write no other and read these).  An append takes the
+ * least one that brings the values of the rows that it puts into a block to at
+ * most 448, drafts that are rejected later among them; a commit the largest of the
+ * blocks that its rows come from; and it never falls while the block holds
+ * committed rows.  So a scale is an upper bound for what its block holds.  A power
+ * of two, so that a scale that is larger than these rows need, or that grows under
+ * them, costs them nothing but the last bits of numbers that become subnormal:
+ * values below 2^(E - 127 - 6) are multiples of 2^(E - 127 - 9), and a cache filled
+ * through rejected drafts may differ in them from one that never saw these.
  *
  * In an ooo_paged_batch for these entry points page_rows is at least 32 and
  * page_stride counts bytes (a multiple of 16); dt is the type of q, qkv, the

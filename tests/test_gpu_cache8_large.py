@@ -1,11 +1,15 @@
 """The 8-bit cache's append past the rows up to which a block's heads are shared out among workgroups
-(csrc/cache8.hip, kFewRows), and compactions over several windows of 256 rows."""
+(csrc/cache8.hip, kFewRows), compactions over several windows of 256 rows, and commits against direct appends."""
 
 import random
 
 import numpy as np
 import pytest
 import torch
+
+from oracle import batch as ob
+from oracle import cache8 as oc
+from paper_2608_00814_amd import ooo
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +97,60 @@ def test_compact_leaves_bad_entries_of_later_windows():
     path, acc = long_paths(r, rows, "sparse")
     path[0, 300], path[0, 400], path[1, 257] = 700, -3, 1 << 30  # not rows: they stay where they are
     check_compact(b, path, acc)
+
+
+def commit(b, qkv, path, acc, depth):
+    q = torch.empty((b.n_rows, b.Hq, b.D), dtype=b.dt, device="cuda")
+    ooo.paged_append8(b.batch, b.cache, qkv, None, None, 1e-6, 1e6, q, depth=torch.from_numpy(depth).cuda())
+    if path is not None:
+        ooo.paged_compact8(b.batch, b.cache, torch.from_numpy(path).cuda(), torch.from_numpy(acc).cuda())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_commit_against_a_direct_append(dt):
+    """A trie appended and its accepted rows committed, against an append of the accepted rows alone.  Rejected rows
+    may leave a larger scale behind (e against e'), never a smaller one.  A number whose size is 2^(e - 6) or more is
+    normal under both scales and so rounded alike.  Any other one is rounded to steps of 2^(e - 9) or finer: when it
+    is appended, again when it is put under e, and in the direct append: 3 2^(e - 10) at most between the two.  (A
+    rotated key may come from another form of the same float32 products: then it may also be the next number.)"""
+    r = random.Random(4)
+    rows, lens, Hkv, D, R = [50, 40, 64, 9, 1], [30, 0, 64, 95, 33], 2, 64, 32
+    mask, depth = bh.trie_masks(r, rows, 1)
+    path, acc = np.full((5, 65), -1, np.int32), np.zeros(5, np.int32)
+    for s, n in enumerate(rows):
+        at = int(np.cumsum([0] + rows)[s])
+        node = max(range(n), key=lambda j: depth[at + j])
+        p = [j for j in range(n) if (int(mask[at + node, 0]) >> j) & 1]
+        path[s, :len(p)], acc[s] = p, len(p) - 1
+    starts = np.cumsum([0] + rows)
+    a = Batch8(dt, 2, Hkv, D, R, rows, lens, shared=20, seed=2, spread=0.3)
+    # sizes from 1 to 1000 for rejected rows, near 1 for the others
+    qkv = sized(a.n_rows, 6 * D, dt, 5)
+    kept = np.concatenate([starts[s] + path[s, :acc[s] + 1] for s in range(5)])
+    x = torch.randn((len(kept), 6 * D), generator=torch.Generator(device="cuda").manual_seed(6), device="cuda")
+    qkv[torch.from_numpy(kept).cuda()] = x.to(a.dt)
+    few = [int(n) + 1 for n in acc]
+    d = Batch8(dt, 2, Hkv, D, R, few, lens, shared=20, seed=2, spread=0.3)
+    d.table = a.table.copy()
+    d.d_table = torch.from_numpy(d.table).cuda()
+    d.k, d.v, d.ks, d.vs = a.k.clone(), a.v.clone(), a.ks.clone(), a.vs.clone()
+    d.bind()
+    commit(a, qkv, path, acc, depth)
+    commit(d, qkv[torch.from_numpy(kept).cuda()].contiguous(), None, None,
+           np.concatenate([np.arange(n, dtype=np.int32) for n in few]))
+    coarser = differ = 0
+    for kv, (ca, sa), (cd, sd) in zip((0, 1), a.bytes(), d.bytes()):
+        va, vd = oc.values(ca, sa), oc.values(cd, sd)
+        for s, n in enumerate(few):
+            for t in range(lens[s] // 32 * 32, lens[s] + n):
+                page, row = ob.place(a.table[s], t, R)
+                e, e1 = (x[page, :, row // 32].astype(int) - 127 for x in (sa, sd))
+                assert (e >= e1).all()
+                up, y, z = np.exp2(e.astype(float))[:, None], va[page, :, row], vd[page, :, row]
+                normal = np.abs(z) >= up * 2.0 ** -6
+                next_ = np.abs(z) / 8 if kv == 0 else 0.0
+                assert kv == 0 or np.array_equal(y[normal], z[normal])
+                assert (np.abs(y - z) <= 3 * up * 2.0 ** -10 + next_).all()
+                coarser += (e > e1).sum()
+                differ += (y != z).sum()
+    assert coarser > 0 and differ > 0
