@@ -246,11 +246,14 @@ __device__ __forceinline__ void append_block(const AppendArgs& a, int task, int 
 // quantise the blocks that begin there (with a sequence's first new row, or a
 // block of its own tokens); the others take four rows of queries each.  Up to
 // kFewRows rows a block's heads go to several workgroups (blockIdx.y), four
-// heads' K or V each: 8 tries of 64 rows took 17.7 us with all heads in one, and
-// take 13.4 so; 10k rows of prompts take 51 with all in one and 59 so.  11760 rows
-// of prompts, 32 heads of 128 and 8 of K and V, take 63 us (264 MB, 4.2 TB/s of the
-// 4.96 of a copy), the queries' part alone 43 and the pages' alone 33.  A row for
-// each of 256 requests: 5.9 us in a graph.
+// heads' K or V each: with 32 heads of 128 and 8 of K and V, 614 rows of four
+// prompts take 12 us so and 20 with all heads in one, 2463 rows 21 and 25, 3197 of
+// eight 23 and 25, 4914 42 and 40, 6399 47 and 42, 11760 of sixteen 70 and 65; with
+// 2 heads of K and V no less or more.  (A row each of 1024 requests takes 18 so and
+// 13 with all in one, of 3000 45 and 28: workgroups that find nothing to do.  Of 64,
+// 6 either way.)  11760 rows of prompts: 63 us (264 MB, 4.2 TB/s of the 4.96 of a
+// copy), the queries' part alone 43 and the pages' alone 33.  A row for each of 256
+// requests: 5.9 us in a graph, 17.7 where every block's scale grows.
 template <class T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void append8_kernel(AppendArgs a, int units) {
   constexpr int HALF = D / 2, SLOTS = 64 / (HALF / Vec16<T>::N);

@@ -91,7 +91,13 @@ constexpr PlanCosts kCosts{21.f, 160.f, 5.f, 0.05f};
 // 8-bit pages: half the bytes of a half-tile, and wide tiles that convert.  256
 // rows over 32k with up to 4k own take 306 us at halves of 3.5 to 4 and shares of
 // HBM of 0.015 to 0.04, and 346 at 2.5, 325 at 4.5 to 7, 328 at a share of 0.05,
-// 690 at a half of 0.5; own keys alone 206 from 0.025 on and 236 at 0.015.
+// 690 at a half of 0.5; own keys alone 206 from 0.025 on and 236 at 0.015.  Of
+// fifteen shapes (32 to 300 rows over up to 32k and 16k own, tries, prompts, heads of
+// 64) these take within 2% of the best of tiles of 21 to 31, halves of 3 to 4.5 and
+// shares of 0.025 to 0.045, but for 64 rows of 40 heads over 12k (50 us; 46 at a tile
+// of 21) and 128 rows over 16k with 4k own (122; 118 at 0.045); a share of 0.025 or
+// 0.045 or a tile of 21 costs 100 rows over 20k with 8k own 11 to 14%, a tile of 31
+// the 256 rows 13%, a half of 4.5 the same at heads of 64 9%; halves of 3 nothing.
 constexpr PlanCosts kCosts8{26.f, 160.f, 3.5f, 0.033f};
 
 // The deal that finishes first, for every lane of a wave, each of which tries
