@@ -120,7 +120,7 @@ def fork(seq_len, table, parent, fresh, n_pages, page_rows, in_place):
         p = int(parent[b])
         if p < 0 or p == b or p >= n or not 0 <= fresh[b] < n_pages or not 0 <= seq_len[p] < ld * page_rows:
             continue
-        if in_place and parent[p] >= 0 and parent[p] != p:
+        if in_place and 0 <= parent[p] < n and parent[p] != p:
             continue
         full, rows = divmod(int(seq_len[p]), page_rows)
         if rows:

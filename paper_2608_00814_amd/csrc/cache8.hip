@@ -434,7 +434,8 @@ __global__ __launch_bounds__(256) void fork_kernel(ForkArgs a) {
     n = a.seq_len[p];
     const int pp = a.parent[p];
     rows = n & ((1 << a.page_shift) - 1);
-    forks = to >= 0 && to < a.n_pages && n >= 0 && n < a.own_cap && !(in_place && pp >= 0 && pp != p);
+    forks = to >= 0 && to < a.n_pages && n >= 0 && n < a.own_cap &&
+            !(in_place && pp >= 0 && pp != p && pp < a.n_seqs);
     if (forks && rows > 0) {
       page = a.table[(size_t)p * a.table_ld + (n >> a.page_shift)];
       forks = page >= 0 && page < a.n_pages;

@@ -1,5 +1,6 @@
 """The 8-bit cache's append past the rows up to which a block's heads are shared out among workgroups
-(csrc/cache8.hip, kFewRows), compactions over several windows of 256 rows, and commits against direct appends."""
+(csrc/cache8.hip, kFewRows), compactions over several windows of 256 rows, commits against direct appends, and
+forks of parents without parents."""
 
 import random
 
@@ -17,7 +18,7 @@ if torch.cuda.is_available():
     import batch_harness as bh
     from batch_harness import TYPES, ragged
     from cache8_harness import Batch8
-    from test_gpu_cache8 import check_compact, run_append
+    from test_gpu_cache8 import Forks, check_compact, run_append
 
 FEW = 4096
 
@@ -154,3 +155,10 @@ def test_commit_against_a_direct_append(dt):
                 coarser += (e > e1).sum()
                 differ += (y != z).sum()
     assert coarser > 0 and differ > 0
+
+
+@pytest.mark.parametrize("kind", ["f8", "bf16"])
+def test_fork_in_place_of_a_parent_whose_own_parent_is_none(kind):
+    """An entry past the sequences names none: its sequence is left as it is, and its children continue it."""
+    f = Forks(kind, [40, 7, 64, 33], 32)
+    assert len(f.check([4, 0, 1 << 30, 2], True)) == 1 and f.d_len.tolist() == [40, 40, 64, 64]
